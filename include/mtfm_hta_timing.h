@@ -31,7 +31,7 @@ enum { MTFM_HTA_KERNEL_FWD = 0,      /* forward attention kernel */
        MTFM_HTA_KERNEL_BWD_DKDV = 3, /* dk, dv of the history and real-time keys (key-stationary pass, one launch or two); of
                                         a call of little work everything but the row statistics, of a call whose users have
                                         few query rows the whole backward pass where one kernel forms it */
-       MTFM_HTA_N_KERNELS = 7        /* kinds 4..6 belong to mtfm_gln.h */ };
+       MTFM_HTA_N_KERNELS = 15       /* kinds 4..6 belong to mtfm_gln.h, 7..9 to mtfm_rms.h, 10..14 to mtfm_hla.h */ };
 MTFM_HTA_API int mtfm_hta_timing_enable(int slots);
 MTFM_HTA_API int mtfm_hta_timing_read(int kernel, float* ms, int capacity);
 

@@ -3,11 +3,13 @@
 // ctypes converts every argument of a foreign call on its own (about 0.15 us each, 4 us for the 28 of an attention call,
 // on top of launches of 2 us); the binding packs the arguments with one struct.pack instead and passes the address.
 // Same checks, kernels, results and error codes as the functions of include/, which these forward to.  The block is
-// read during the call and not kept.  The field order is that of the pack formats in hta.py and gln.py: pointers, then
+// read during the call and not kept.  The field order is that of the pack formats in hta.py, gln.py, hla.py and rms.py: pointers, then
 // 8-byte, then 4-byte fields, nothing padded.
 #include "../../include/mtfm_gln.h"
+#include "../../include/mtfm_hla.h"
 #include "../../include/mtfm_hta.h"
 #include "../../include/mtfm_hta_pw.h"
+#include "../../include/mtfm_rms.h"
 #include "hta_common.h"
 
 namespace {
@@ -45,6 +47,52 @@ struct GlnArgs {
     int32_t dtype;
 };
 static_assert(sizeof(GlnArgs) == 14 * 8 + 3 * 8 + 4 * 4, "pack format 14P3q2ifi");
+
+struct HlaArgs {
+    const void *q, *k, *v;
+    void* out;
+    const float *log_decay, *state;
+    float* final_state;
+    const void* dout;
+    void *dq, *dk, *dv;
+    const float* dfinal_state;
+    float* dstate;
+    const int32_t *q_offsets, *kv_offsets, *hist_len, *n_targets;
+    void* workspace;
+    int64_t workspace_bytes, total_q, total_kv;
+    int32_t batch, max_hist, max_targets, Hq, Hkv, head_dim;
+    float scale;
+    int32_t dtype, layer, backward;
+};
+static_assert(sizeof(HlaArgs) == 18 * 8 + 3 * 8 + 10 * 4, "pack format 18P3q6if3i");
+
+struct HlaStepArgs {
+    const void *q, *k, *v;
+    const float *log_decay, *state;
+    float* new_state;
+    const int32_t* slots;
+    void* out;
+    int32_t n_rows, n_slots, Hq, Hkv, head_dim;
+    float scale;
+    int32_t dtype, unused;
+};
+static_assert(sizeof(HlaStepArgs) == 8 * 8 + 8 * 4, "pack format 8P5if2i");
+
+enum RmsCall { RMS_FWD = 0, RMS_FWD_Q8 = 1, RMS_BWD = 2 };
+struct RmsArgs {
+    const void *x, *residual;  // backward: h, dh
+    const float* weight;
+    void *h, *y;               // y: also the result in 8 bits; backward: dx
+    float *rstd, *scale;
+    const void* dy;
+    float* dweight;
+    void* workspace;
+    int64_t x_stride, residual_stride, dy_stride, n_rows, workspace_bytes;
+    int32_t width;
+    float eps;
+    int32_t dtype, kind, call, unused;
+};
+static_assert(sizeof(RmsArgs) == 10 * 8 + 5 * 8 + 6 * 4, "pack format 10P5qif4i");
 
 // what the host knows of a bf16 call; false: no such call
 bool sizes_of(const HtaArgs& a, hta::Params& p) {
@@ -145,6 +193,39 @@ MTFM_HTA_API int mtfm_binding_gln(const void* block, void* stream) {
                             a.eps, a.dtype, stream);
     return mtfm_gln_bwd(a.dy, a.x, a.gate, a.group_id, a.gamma, a.beta, a.mean, a.rstd, a.dx, a.dgate, a.dgamma, a.dbeta,
                         a.n_tokens, a.d_model, a.n_groups, a.dtype, a.workspace, (size_t)a.workspace_bytes, stream);
+}
+
+MTFM_HTA_API int mtfm_binding_hla(const void* block, void* stream) {
+    const HlaArgs& a = *(const HlaArgs*)block;
+    const size_t ws = (size_t)a.workspace_bytes;
+    if (!a.backward)
+        return mtfm_hla_fwd(a.q, a.k, a.v, a.log_decay, a.state, a.out, a.final_state, a.q_offsets, a.kv_offsets, a.hist_len, a.n_targets, a.batch,
+                            a.total_q, a.total_kv, a.max_hist, a.max_targets, a.Hq, a.Hkv, a.head_dim, a.scale, a.dtype, a.layer, a.workspace, ws,
+                            stream);
+    return mtfm_hla_bwd(a.dout, a.q, a.k, a.v, a.log_decay, a.state, a.dfinal_state, a.dq, a.dk, a.dv, a.dstate, a.q_offsets, a.kv_offsets,
+                        a.hist_len, a.n_targets, a.batch, a.total_q, a.total_kv, a.max_hist, a.max_targets, a.Hq, a.Hkv, a.head_dim, a.scale, a.dtype,
+                        a.layer, a.workspace, ws, stream);
+}
+
+MTFM_HTA_API int mtfm_binding_hla_step(const void* block, void* stream) {
+    const HlaStepArgs& a = *(const HlaStepArgs*)block;
+    return mtfm_hla_step(a.q, a.k, a.v, a.log_decay, a.state, a.new_state, a.slots, a.out, a.n_rows, a.n_slots, a.Hq, a.Hkv, a.head_dim, a.scale,
+                         a.dtype, stream);
+}
+
+MTFM_HTA_API int mtfm_binding_rms(const void* block, void* stream) {
+    const RmsArgs& a = *(const RmsArgs*)block;
+    switch (a.call) {
+        case RMS_FWD:
+            return mtfm_rms_fwd(a.x, a.x_stride, a.residual, a.residual_stride, a.weight, a.h, a.y, a.rstd, a.n_rows, a.width, a.eps, a.dtype,
+                                stream);
+        case RMS_FWD_Q8:
+            return mtfm_rms_fwd_q8(a.x, a.x_stride, a.residual, a.residual_stride, a.weight, a.h, a.y, a.scale, a.n_rows, a.width, a.eps, a.dtype,
+                                   a.kind, stream);
+        default:
+            return mtfm_rms_bwd(a.dy, a.dy_stride, a.x, a.x_stride, a.weight, a.rstd, a.residual, a.residual_stride, a.y, a.dweight, a.n_rows,
+                                a.width, a.dtype, a.workspace, (size_t)a.workspace_bytes, stream);
+    }
 }
 
 }  // extern "C"

@@ -94,11 +94,27 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _device_index = getattr(torch._C, "_cuda_getDevice", None)
 
 
+def check_on_current_device(*tensors) -> None:
+    """Kernels run on the current GPU, and so must all tensors (None: one that is not there) lie."""
+    for t in tensors:
+        if t is not None and t.get_device() < 0:
+            raise ValueError(f"all tensors must be on the current GPU, got one on {t.device}")
+    here = torch.cuda.current_device() if _device_index is None else _device_index()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"all tensors must be on the current GPU ({here}), got one on {t.device}")
+
+
 def _current_stream() -> int:
     """Handle of the current stream of the current device."""
     if _raw_stream is None or _device_index is None:
         return torch.cuda.current_stream().cuda_stream
     return _raw_stream(_device_index())
+
+
+def _address(t: Optional[torch.Tensor]) -> int:
+    """Device address for a packed block; 0 for None."""
+    return 0 if t is None else t.data_ptr()
 
 
 def _stream_handle(stream) -> Optional[int]:
