@@ -22,7 +22,8 @@
  * float32, 16-byte aligned.  final_state may be `state` itself, and dstate dfinal_state; other outputs overlap nothing.
  * Products take bf16 operands with float32 sums; the running state is float32, and what enters it is rounded no further than
  * to 16 bits of significand.  Rows that belong to no user (behind the last one's, or beyond hist_len + n_targets) are not
- * touched.  What a row may not see does not reach it, whatever it holds (infinities, NaN).
+ * touched.  What a row may not see does not reach it, whatever it holds; what sees an infinity or a NaN is not finite (and may be
+ * NaN where the formula gives an infinity).  Hq * head_dim at most 2^22.
  *
  * Pointers are DEVICE pointers owned by the caller; `stream` is a hipStream_t passed as void* (NULL = the default stream).  The
  * calls validate their scalar arguments on the host, enqueue kernels and return; they never allocate, copy to the host or

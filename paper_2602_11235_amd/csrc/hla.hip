@@ -51,13 +51,17 @@ struct Args {
 __device__ inline floatx4 mfma16(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
-// is any of eight values infinite or NaN?  (an exponent of all ones carries into the sign)
-__device__ inline unsigned nonfinite(bf16x8 x) {
-    const uintx4 u = __builtin_bit_cast(uintx4, x);
-    unsigned r = 0;
+// Eight float32 values as the sum of two bf16 ones: the upper half of each as it stands, and what that leaves off, rounded
+__device__ inline void split8(const float (&x)[8], bf16x8& hi, bf16x8& lo) {
+    uintx4 h;
 #pragma unroll
-    for (int i = 0; i < 4; i++) r |= (u[i] & 0x7F807F80u) + 0x00800080u;
-    return r & 0x80008000u;
+    for (int e = 0; e < 4; e++) {
+        const unsigned a = __builtin_bit_cast(unsigned, x[2 * e]), b = __builtin_bit_cast(unsigned, x[2 * e + 1]);
+        h[e] = __builtin_amdgcn_perm(b, a, 0x07060302);
+        lo[2 * e] = (__bf16)(x[2 * e] - __builtin_bit_cast(float, a & 0xFFFF0000u));
+        lo[2 * e + 1] = (__bf16)(x[2 * e + 1] - __builtin_bit_cast(float, b & 0xFFFF0000u));
+    }
+    hi = __builtin_bit_cast(bf16x8, h);
 }
 
 // Where a user's rows lie, whatever the arrays hold: inside the tensors
@@ -77,56 +81,58 @@ __device__ inline User user_of(const Args& g, int u) {
     return r;
 }
 
-// One sweep over a user by a workgroup of D / 16 waves.  Forwards a workgroup has one query head, backwards G heads of a group, whose outputs
+// waves per SIMD that the registers are to leave room for
+constexpr int sweep_waves(int D, int G, int CB) { return D == 32 && G == 1 ? 4 : D * G * CB <= 64 ? 3 : 2; }
+
+// One sweep over a user by a workgroup of D / (16 CB) waves, each with CB blocks of 16 columns.  Forwards a workgroup has one query head, backwards G heads of a group, whose outputs
 // (dv or dk of their common key/value head) it sums.  D[m][n] += A[m][k] B[k][n] of 16x16x32: a lane holds row (column) lane % 16 and k = 8 (lane / 16) ..
 // + 7 of either operand, and column lane % 16, rows 4 (lane / 16) .. + 3 of the result.
-template <int D, int G, bool BACK>
-__global__ __launch_bounds__(D * 4, G * D <= 64 ? 4 : 2) void sweep_kernel(const Args args) {
-    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, KS = D / 32, LOADS = CHUNK * C16 / NT;
-    static_assert(LOADS == 2, "two 16-byte words of each tile to a thread");
+template <int D, int G, int CB, bool BACK>
+__global__ __launch_bounds__(D * 4 / CB, sweep_waves(D, G, CB)) void sweep_kernel(const Args args) {
+    constexpr int NW = D / 16 / CB, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = CHUNK / PART;  // PART: rows that the threads load at a time
     __shared__ __attribute__((aligned(16))) __bf16 a_s[CHUNK * D], b_s[CHUNK * D], c_s[CHUNK * D], p_s[CHUNK * CHUNK];
     __shared__ float dots_s[CHUNK];
+    // powers of the heads' decays, as they are and times `scale`: entry ZERO + m holds l^m, m = -64 .. 64, 0 for m < 0
+    constexpr int ZERO = CHUNK, POWERS = 2 * CHUNK + 4;
+    __shared__ float power_s[G][POWERS], scaled_s[G][POWERS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
 
     // which user, heads and pass: those that share rows are neighbours on one XCD
-    const int members = (BACK ? args.spread : args.ratio) * args.n_pass;
+    const int per_pass = BACK ? args.spread : args.ratio, members = per_pass * args.n_pass;
     const int xcd = blockIdx.x % hta::N_XCD, slot = blockIdx.x / hta::N_XCD;
     const int group = (slot / members) * hta::N_XCD + xcd, member = slot % members;
     if (group >= args.batch * args.Hkv) return;
-    const int u = group / args.Hkv, kvh = group % args.Hkv, sub = member % (members / args.n_pass);
-    const Pass& ps = args.pass[member / (members / args.n_pass)];
+    const int u = group / args.Hkv, kvh = group % args.Hkv, sub = member % per_pass;
+    const Pass ps = args.pass[member / per_pass];
     const int qh0 = kvh * args.ratio + sub * G;  // the first of the G query heads
     const User us = user_of(args, u);
     const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK, chunks = nh + nt;
     const bool full = args.full;
 
-    float g2[G];
-#pragma unroll
-    for (int g = 0; g < G; g++) g2[g] = fmaxf(fminf(args.log_decay[qh0 + g], 0.f) * hta::LOG2E, MIN_LOG2);
-
-    // state: tile t of head g, register v: row 32 (t / 2) + 8 quad + 4 (t % 2) + v, column 16 wave + l16.  (Rows in this order make the accumulators of
+    // state: tile t of head g and block b, register v: row 32 (t / 2) + 8 quad + 4 (t % 2) + v, column 16 (CB wave + b) + l16.  (Rows in this order make the accumulators of
     // two tiles eight consecutive rows: what an operand wants.)
-    floatx4 S[G][2 * KS];
-    const int col = 16 * wave + l16;
+    floatx4 S[G][CB][2 * KS];
 #pragma unroll
     for (int g = 0; g < G; g++) {
         const float* in = ps.state_in ? ps.state_in + ((int64_t)u * args.Hq + qh0 + g) * D * D : nullptr;
 #pragma unroll
-        for (int t = 0; t < 2 * KS; t++) {
-            const int row = 32 * (t / 2) + 8 * quad + 4 * (t % 2);
-            S[g][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-            if (in) {
-                if (ps.transposed) S[g][t] = *(const floatx4*)(in + col * D + row);
-                else
+        for (int b = 0; b < CB; b++)
 #pragma unroll
-                    for (int v = 0; v < 4; v++) S[g][t][v] = in[(row + v) * D + col];
+            for (int t = 0; t < 2 * KS; t++) {
+                const int row = 32 * (t / 2) + 8 * quad + 4 * (t % 2), col = 16 * (CB * wave + b) + l16;
+                S[g][b][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+                if (in) {
+                    if (ps.transposed) S[g][b][t] = *(const floatx4*)(in + col * D + row);
+                    else
+#pragma unroll
+                        for (int v = 0; v < 4; v++) S[g][b][t][v] = in[(row + v) * D + col];
+                }
             }
-        }
     }
 
-    struct Rows {  // of a chunk: n rows, first + r (backwards through a history: first - r)
+    struct Rows {  // of a chunk: n rows, row r is first + r (backwards through a history: first - r)
         int64_t q, kv;
-        int n, step;
+        int n;
         bool hist;
     };
     const auto rows_of = [&](int c) {
@@ -134,46 +140,59 @@ __global__ __launch_bounds__(D * 4, G * D <= 64 ? 4 : 2) void sweep_kernel(const
         r.hist = BACK ? c >= nt : c < nh;
         if (r.hist) {
             const int first = (BACK ? c - nt : c) * CHUNK, at = BACK ? us.L - 1 - first : first;
-            r.n = min(CHUNK, us.L - first), r.step = BACK ? -1 : 1;
+            r.n = min(CHUNK, us.L - first);
             r.kv = us.kv0 + at, r.q = us.q0 + at;
         } else {
             const int first = (BACK ? c : c - nh) * CHUNK;
-            r.n = min(CHUNK, us.T - first), r.step = 1;
+            r.n = min(CHUNK, us.T - first);
             r.kv = us.kv0 + us.L + first, r.q = us.q0 + (full ? us.L : 0) + first;
         }
         return r;
     };
-    // 16-byte words of the three tiles on their way: word tid + i NT of a tile is word % C16 of row / C16.  Rows that are not there are zero.
+    // A chunk's rows in memory: a uniform address, that of its lowest of 64 rows (backwards through a history row 63, which need not be there), and a
+    // lane's bytes from there
+    const int heads_a = BACK ? args.Hkv : args.Hq, heads_b = BACK ? args.Hq : args.Hkv;
+    const unsigned pitch_a = heads_a * (D * 2), pitch_b = heads_b * (D * 2);
+    const auto lowest = [](bool down, int64_t first) { return down ? first - (CHUNK - 1) : first; };
+    const auto bytes_of = [](bool down, int r, unsigned pitch, int byte) { return __umul24(down ? CHUNK - 1 - r : r, pitch) + byte; };
+
+    // 16-byte words of the three tiles on their way: word tid % C16 of rows tid / C16 + i PART.  Rows that are not there are zero.
+    const int row_t = tid / C16, word_t = tid % C16;
     bf16x8 av[LOADS], bv[LOADS], cv[LOADS];
-    const auto fetch = [&](int c, int g) {
-        const Rows r = rows_of(c);
+    const auto fetch = [&](int chunk, int g) {
+        const Rows r = rows_of(chunk);
         const bool asks = full || !r.hist;  // are there query rows?
-        const bool has_a = (BACK || asks) && (G == 1 || g == 0), has_bc = !BACK || asks;
-        const int heads_a = BACK ? args.Hkv : args.Hq, heads_b = BACK ? args.Hq : args.Hkv;
+        const bool has_a = (BACK || asks) && (G == 1 || g == 0), has_bc = !BACK || asks, down = BACK && r.hist;
         const int head_a = BACK ? kvh : qh0, head_b = BACK ? qh0 + g : kvh;
-        const int64_t row_a = BACK ? r.kv : r.q, row_b = BACK ? r.q : r.kv;
+        const int64_t row_b = lowest(down, BACK ? r.q : r.kv) * heads_b + head_b;
+        const char* a = (const char*)(ps.a + (lowest(down, BACK ? r.kv : r.q) * heads_a + head_a) * D);
+        const char *b = (const char*)(ps.b + row_b * D), *c = (const char*)(ps.c + row_b * D);
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
-            const int row = (tid + i * NT) / C16, word = (tid + i * NT) % C16;
+            const int row = row_t + i * PART;
             const bool there = row < r.n;
+            const unsigned at_a = bytes_of(down, row, pitch_a, word_t * 16), at_b = bytes_of(down, row, pitch_b, word_t * 16);
             av[i] = bv[i] = cv[i] = bf16x8{};
-            if (there && has_a) av[i] = *(const bf16x8*)(ps.a + ((row_a + r.step * row) * heads_a + head_a) * D + word * 8);
-            if (there && has_bc) {
-                bv[i] = *(const bf16x8*)(ps.b + ((row_b + r.step * row) * heads_b + head_b) * D + word * 8);
-                cv[i] = *(const bf16x8*)(ps.c + ((row_b + r.step * row) * heads_b + head_b) * D + word * 8);
-            }
+            if (there && has_a) av[i] = *(const bf16x8*)(a + at_a);
+            if (there && has_bc) bv[i] = *(const bf16x8*)(b + at_b), cv[i] = *(const bf16x8*)(c + at_b);
         }
     };
     const auto word_at = [](const __bf16* tile, int row, int word) { return tile + row * D + ((word ^ swizzle<D>(row)) * 8); };
 
     if (chunks > 0) fetch(0, 0);
+    for (int i = tid; i < G * POWERS; i += NT) {
+        const int g = i / POWERS, m = i % POWERS - ZERO;
+        const float g2 = fmaxf(fminf(args.log_decay[qh0 + g], 0.f) * hta::LOG2E, MIN_LOG2);
+        const float p = m < 0 ? 0.f : fast_exp2(g2 * (float)m);
+        power_s[g][m + ZERO] = p, scaled_s[g][m + ZERO] = p * args.scale;
+    }
     // (entries of P that a product reads and no chunk writes)
     for (int i = tid; i < CHUNK * CHUNK / 8; i += NT) ((bf16x8*)p_s)[i] = bf16x8{};
 
-    floatx4 acc[4];
+    floatx4 acc[CB][4];
     for (int c = 0; c < chunks; c++) {
         const Rows r = rows_of(c);
-        const bool asks = full || !r.hist;
+        const bool asks = full || !r.hist, down = BACK && r.hist;
         const bool has_out = BACK || asks, has_bc = !BACK || asks;
         const bool intra = r.hist && has_out && has_bc, inter = r.hist ? has_out : !BACK, update = r.hist ? has_bc : BACK;
 #pragma unroll
@@ -181,145 +200,199 @@ __global__ __launch_bounds__(D * 4, G * D <= 64 ? 4 : 2) void sweep_kernel(const
             // (the last readers of the tiles are behind the barrier at the end of the turn)
 #pragma unroll
             for (int i = 0; i < LOADS; i++) {
-                const int row = (tid + i * NT) / C16, word = (tid + i * NT) % C16;
-                if (g == 0) *(bf16x8*)word_at(a_s, row, word) = av[i];
-                *(bf16x8*)word_at(b_s, row, word) = bv[i];
-                *(bf16x8*)word_at(c_s, row, word) = cv[i];
+                if (g == 0) *(bf16x8*)word_at(a_s, row_t + i * PART, word_t) = av[i];
+                *(bf16x8*)word_at(b_s, row_t + i * PART, word_t) = bv[i];
+                *(bf16x8*)word_at(c_s, row_t + i * PART, word_t) = cv[i];
             }
             __syncthreads();
             if (g + 1 < G) fetch(c, g + 1);
             else if (c + 1 < chunks) fetch(c + 1, 0);
 
-            if (g == 0)
-#pragma unroll
-                for (int it = 0; it < 4; it++) acc[it] = floatx4{0.f, 0.f, 0.f, 0.f};
-            floatx4 from_state[4];
-#pragma unroll
-            for (int it = 0; it < 4; it++) from_state[it] = floatx4{0.f, 0.f, 0.f, 0.f};
             if (intra) {
                 // P^T = B A^T with the decays, tiles on and below the diagonal, dealt to the waves
-                for (int t = wave; t < 10; t += NW) {
+#pragma unroll
+                for (int t0 = 0; t0 < 10; t0 += NW) {
+                    const int t = t0 + wave;
+                    if (t >= 10) break;
                     const int it = t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, jt = t - it * (it + 1) / 2;
+                    const int i = 16 * it + l16, j = 16 * jt + 4 * quad;
                     floatx4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int k = 0; k < KS; k++)
-                        s = mfma16(*(const bf16x8*)word_at(b_s, 16 * jt + l16, 4 * k + quad), *(const bf16x8*)word_at(a_s, 16 * it + l16, 4 * k + quad), s);
-                    const int i = 16 * it + l16, j = 16 * jt + 4 * quad;
+                        s = mfma16(*(const bf16x8*)word_at(b_s, 16 * jt + l16, 4 * k + quad), *(const bf16x8*)word_at(a_s, i, 4 * k + quad), s);
+                    float w[4];
+                    const float* power = scaled_s[g] + ZERO + i - j;
+#pragma unroll
+                    for (int v = 0; v < 4; v++) w[v] = power[-v];
                     bf16x4 p;
 #pragma unroll
-                    for (int v = 0; v < 4; v++)
-                        p[v] = (__bf16)(i >= j + v ? s[v] * (args.scale * fast_exp2(g2[g] * (float)(i - j - v))) : 0.f);
+                    for (int v = 0; v < 4; v++) {
+                        s[v] *= w[v];
+                        p[v] = (__bf16)(i - j >= v ? s[v] : 0.f);  // (0 times what a later row holds need not be 0)
+                    }
                     *(bf16x4*)(p_s + i * CHUNK + (((j / 8) ^ swizzle<64>(i)) * 8) + (j & 4)) = p;
                 }
             } else if (!r.hist) {
-                // own keys only: <a_i, b_i>, D / 16 lanes to a row
+                // own keys only: <a_i, b_i>, NW lanes to a row
                 const int row = tid / NW, part = tid % NW;
                 float dot = 0.f;
 #pragma unroll
-                for (int k = 0; k < 2; k++) dot = hta::dot_bf16x8(dot, *(const bf16x8*)word_at(a_s, row, 2 * part + k), *(const bf16x8*)word_at(b_s, row, 2 * part + k));
+                for (int k = 0; k < C16 / NW; k++)
+                    dot = hta::dot_bf16x8(dot, *(const bf16x8*)word_at(a_s, row, C16 / NW * part + k), *(const bf16x8*)word_at(b_s, row, C16 / NW * part + k));
                 dot = hta::sum_lanes<NW>(dot);
                 if (part == 0) dots_s[row] = dot * args.scale;
             }
+            // o^T = S^T A^T, row i of it times l^(i+1) scale (candidates: l scale, backwards: l^i)
+            floatx4 o[CB][4];
             if (inter) {
-                // o^T = S^T A^T
+                bf16x8 s[CB][KS];
 #pragma unroll
-                for (int k = 0; k < KS; k++) {
-                    bf16x8 s;
+                for (int b = 0; b < CB; b++)
 #pragma unroll
-                    for (int v = 0; v < 4; v++) s[v] = (__bf16)S[g][2 * k][v], s[4 + v] = (__bf16)S[g][2 * k + 1][v];
+                    for (int k = 0; k < KS; k++)
 #pragma unroll
-                    for (int it = 0; it < 4; it++) from_state[it] = mfma16(s, *(const bf16x8*)word_at(a_s, 16 * it + l16, 4 * k + quad), from_state[it]);
-                }
+                        for (int v = 0; v < 4; v++) s[b][k][v] = (__bf16)S[g][b][2 * k][v], s[b][k][4 + v] = (__bf16)S[g][b][2 * k + 1][v];
 #pragma unroll
-                for (int it = 0; it < 4; it++) {
-                    const float f = BACK ? fast_exp2(g2[g] * (float)(16 * it + l16)) : args.scale * fast_exp2(g2[g] * (float)(r.hist ? 16 * it + l16 + 1 : 1));
+                for (int it = 0; it < 4; it++)
 #pragma unroll
-                    for (int v = 0; v < 4; v++) acc[it][v] += from_state[it][v] * f;
-                }
+                    for (int k = 0; k < KS; k++) {
+                        const bf16x8 a = *(const bf16x8*)word_at(a_s, 16 * it + l16, 4 * k + quad);
+#pragma unroll
+                        for (int b = 0; b < CB; b++) o[b][it] = mfma16(s[b][k], a, k == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : o[b][it]);
+                    }
             }
             __syncthreads();
             // C^T: this wave's columns of c, rows 32 k + 8 quad .. + 7
-            bf16x8 ct[2];
+            bf16x8 ct[CB][2];
 #pragma unroll
-            for (int k = 0; k < 2; k++) {
-                const int row = 32 * k + 8 * quad + (l16 >> 2), word = 2 * wave + ((l16 & 3) >> 1), off = (l16 & 1) * 4;
-                ct[k] = hta::lds_read_tr_pair(word_at(c_s, row, word) + off, word_at(c_s, row + 4, word) + off);
-            }
-            const bool odd = __ballot((nonfinite(ct[0]) | nonfinite(ct[1])) != 0) != 0;
+            for (int b = 0; b < CB; b++)
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    const int row = 32 * k + 8 * quad + (l16 >> 2), word = 2 * (CB * wave + b) + ((l16 & 3) >> 1), off = (l16 & 1) * 4;
+                    ct[b][k] = hta::lds_read_tr_pair(word_at(c_s, row, word) + off, word_at(c_s, row + 4, word) + off);
+                }
+            floatx4 within[CB][4];
+#pragma unroll
+            for (int b = 0; b < CB; b++)
+#pragma unroll
+                for (int it = 0; it < 4; it++) within[b][it] = floatx4{0.f, 0.f, 0.f, 0.f};
             if (intra) {
-                if (!odd) {
 #pragma unroll
-                    for (int it = 0; it < 4; it++)
+                for (int it = 0; it < 4; it++)
 #pragma unroll
-                        for (int k = 0; k <= it / 2; k++) {
-                            const int i = 16 * it + l16;
-                            acc[it] = mfma16(ct[k], *(const bf16x8*)(p_s + i * CHUNK + (((4 * k + quad) ^ swizzle<64>(i)) * 8)), acc[it]);
-                        }
-                } else {
-                    // an infinity or a NaN would reach the rows in front of it as 0 times itself: row by row
+                    for (int k = 0; k <= it / 2; k++) {
+                        const int i = 16 * it + l16;
+                        const bf16x8 p = *(const bf16x8*)(p_s + i * CHUNK + (((4 * k + quad) ^ swizzle<64>(i)) * 8));
+#pragma unroll
+                        for (int b = 0; b < CB; b++) within[b][it] = mfma16(ct[b][k], p, within[b][it]);
+                    }
+                // An infinity or a NaN in c reaches the rows in front of it as 0 times itself, and the last rows in any case: then row by row.
+                float zero = 0.f;
+#pragma unroll
+                for (int b = 0; b < CB; b++)
+#pragma unroll
+                    for (int v = 0; v < 4; v++) zero = fmaf(within[b][3][v], 0.f, zero);
+                if (__ballot(zero != zero) != 0) {
+#pragma unroll
+                    for (int b = 0; b < CB; b++)
+#pragma unroll
+                        for (int it = 0; it < 4; it++) within[b][it] = floatx4{0.f, 0.f, 0.f, 0.f};
                     for (int j = 0; j < CHUNK; j++) {
-                        const bf16x4 cj = *(const bf16x4*)(word_at(c_s, j, 2 * wave + (quad >> 1)) + (quad & 1) * 4);
 #pragma unroll
-                        for (int it = 0; it < 4; it++) {
-                            const int i = 16 * it + l16;
-                            const float p = (float)p_s[i * CHUNK + (((j / 8) ^ swizzle<64>(i)) * 8) + (j & 7)];
+                        for (int b = 0; b < CB; b++) {
+                            const bf16x4 cj = *(const bf16x4*)(word_at(c_s, j, 2 * (CB * wave + b) + (quad >> 1)) + (quad & 1) * 4);
 #pragma unroll
-                            for (int v = 0; v < 4; v++) acc[it][v] += j <= i ? p * (float)cj[v] : 0.f;
+                            for (int it = 0; it < 4; it++) {
+                                const int i = 16 * it + l16;
+                                const float p = (float)p_s[i * CHUNK + (((j / 8) ^ swizzle<64>(i)) * 8) + (j & 7)];
+#pragma unroll
+                                for (int v = 0; v < 4; v++) within[b][it][v] += j <= i ? p * (float)cj[v] : 0.f;
+                            }
                         }
                     }
                 }
             } else if (!r.hist) {
 #pragma unroll
-                for (int it = 0; it < 4; it++) {
-                    const int i = 16 * it + l16;
-                    const bf16x4 ci = *(const bf16x4*)(word_at(c_s, i, 2 * wave + (quad >> 1)) + (quad & 1) * 4);
+                for (int b = 0; b < CB; b++)
 #pragma unroll
-                    for (int v = 0; v < 4; v++) acc[it][v] += dots_s[i] * (float)ci[v];
+                    for (int it = 0; it < 4; it++) {
+                        const int i = 16 * it + l16;
+                        const bf16x4 ci = *(const bf16x4*)(word_at(c_s, i, 2 * (CB * wave + b) + (quad >> 1)) + (quad & 1) * 4);
+#pragma unroll
+                        for (int v = 0; v < 4; v++) within[b][it][v] = dots_s[i] * (float)ci[v];
+                    }
+            }
+            if (inter) {
+                const float* power = r.hist ? (BACK ? power_s[g] + ZERO : scaled_s[g] + ZERO + 1) + l16 : scaled_s[g] + ZERO + 1;
+                const int step = r.hist ? 16 : 0;
+#pragma unroll
+                for (int it = 0; it < 4; it++) {
+                    const float f = power[it * step];
+#pragma unroll
+                    for (int b = 0; b < CB; b++)
+#pragma unroll
+                        for (int v = 0; v < 4; v++) within[b][it][v] = fmaf(o[b][it][v], f, within[b][it][v]);
                 }
             }
+#pragma unroll
+            for (int b = 0; b < CB; b++)
+#pragma unroll
+                for (int it = 0; it < 4; it++) acc[b][it] = g == 0 ? within[b][it] : acc[b][it] + within[b][it];
             if (has_out && g == G - 1) {
-                const int heads = BACK ? args.Hkv : args.Hq, head = BACK ? kvh : qh0;
+                const int64_t base = (lowest(down, BACK ? r.kv : r.q) * heads_a + (BACK ? kvh : qh0)) * D;
+                char* out = (char*)(ps.out + base);
+                char* partial = (char*)(ps.partial + (int64_t)sub * args.total_kv * args.Hkv * D + base);
 #pragma unroll
                 for (int it = 0; it < 4; it++) {
-                    const int i = 16 * it + l16;
-                    if (i < r.n) {
-                        const int64_t at = (((BACK ? r.kv : r.q) + r.step * i) * heads + head) * D + 16 * wave + 4 * quad;
-                        if (BACK && ps.partial) {
-                            *(floatx4*)(ps.partial + (int64_t)sub * args.total_kv * args.Hkv * D + at) = acc[it];
-                        } else {
-                            bf16x4 o;
+                    if (16 * it + l16 < r.n) {
+                        const unsigned at = bytes_of(down, 16 * it + l16, pitch_a, (16 * CB * wave + 4 * quad) * 2);
 #pragma unroll
-                            for (int v = 0; v < 4; v++) o[v] = (__bf16)acc[it][v];
-                            *(bf16x4*)(ps.out + at) = o;
+                        for (int b = 0; b < CB; b++) {
+                            if (BACK && ps.partial) {
+                                *(floatx4*)(partial + 2 * at + 64 * b) = acc[b][it];
+                            } else {
+                                bf16x4 x;
+#pragma unroll
+                                for (int v = 0; v < 4; v++) x[v] = (__bf16)acc[b][it][v];
+                                *(bf16x4*)(out + at + 32 * b) = x;
+                            }
                         }
                     }
                 }
             }
             // the state behind the chunk: l^n S + B^T (w c), where w c goes in two halves of 8 bits each, so that float32 keeps 16 of it
             if (r.hist) {
-                const float keep = fast_exp2(g2[g] * (float)r.n);
+                const float keep = power_s[g][ZERO + r.n];
 #pragma unroll
-                for (int t = 0; t < 2 * KS; t++) S[g][t] *= keep;
+                for (int b = 0; b < CB; b++)
+#pragma unroll
+                    for (int t = 0; t < 2 * KS; t++) S[g][b][t] *= keep;
             }
             if (update) {
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
-                    bf16x8 hi, lo;
+                    bf16x8 hi[CB], lo[CB];
+                    float w[8];
+                    // l^(n-1-j) (backwards l^(n-j) scale); rows that are not there are zero, and so are these behind the table's end
+                    const float* p = (BACK ? scaled_s[g] + ZERO + r.n : power_s[g] + ZERO + r.n - 1) - (32 * k + 8 * quad);
 #pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        const int left = r.n - (BACK ? 0 : 1) - (32 * k + 8 * quad + e);
-                        float w = fast_exp2(g2[g] * (float)(r.hist ? left : 1));
-                        if (BACK) w *= args.scale;
-                        const float x = left >= 0 ? w * (float)ct[k][e] : 0.f;  // (rows that are not there)
-                        hi[e] = (__bf16)x;
-                        lo[e] = odd ? (__bf16)0.f : (__bf16)(x - (float)hi[e]);
+                    for (int e = 0; e < 8; e++) w[e] = r.hist ? p[-e] : scaled_s[g][ZERO + 1];
+#pragma unroll
+                    for (int b = 0; b < CB; b++) {
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; e++) x[e] = w[e] * (float)ct[b][k][e];
+                        split8(x, hi[b], lo[b]);
                     }
 #pragma unroll
                     for (int t = 0; t < 2 * KS; t++) {
                         const int row = 32 * k + 8 * quad + (l16 >> 2), word = 4 * (t / 2) + (l16 & 3), off = 4 * (t % 2);
                         const bf16x8 bt = hta::lds_read_tr_pair(word_at(b_s, row, word) + off, word_at(b_s, row + 4, word) + off);
-                        S[g][t] = mfma16(bt, hi, S[g][t]);
-                        S[g][t] = mfma16(bt, lo, S[g][t]);
+#pragma unroll
+                        for (int b = 0; b < CB; b++) {
+                            S[g][b][t] = mfma16(bt, hi[b], S[g][b][t]);
+                            S[g][b][t] = mfma16(bt, lo[b], S[g][b][t]);
+                        }
                     }
                 }
             }
@@ -331,9 +404,11 @@ __global__ __launch_bounds__(D * 4, G * D <= 64 ? 4 : 2) void sweep_kernel(const
         for (int g = 0; g < G; g++) {
             float* out = ps.state_out + ((int64_t)u * args.Hq + qh0 + g) * D * D;
 #pragma unroll
-            for (int t = 0; t < 2 * KS; t++)
+            for (int b = 0; b < CB; b++)
 #pragma unroll
-                for (int v = 0; v < 4; v++) out[(32 * (t / 2) + 8 * quad + 4 * (t % 2) + v) * D + col] = S[g][t][v];
+                for (int t = 0; t < 2 * KS; t++)
+#pragma unroll
+                    for (int v = 0; v < 4; v++) out[(32 * (t / 2) + 8 * quad + 4 * (t % 2) + v) * D + 16 * (CB * wave + b) + l16] = S[g][b][t][v];
         }
     }
 }
@@ -433,6 +508,7 @@ int check_heads(int32_t Hq, int32_t Hkv, int32_t d, int dtype) {
     if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0) return hta::report_error(MTFM_HTA_ERR_INVALID_ARG, "Hq (%d) must be a positive multiple of Hkv (%d)", Hq, Hkv);
     if (d <= 0) return hta::report_error(MTFM_HTA_ERR_INVALID_ARG, "head_dim must be positive, got %d", d);
     if (d != 32 && d != 64 && d != 128) return hta::report_error(MTFM_HTA_ERR_UNSUPPORTED, "head_dim %d: linear attention takes 32, 64 and 128", d);
+    if ((int64_t)Hq * d > 1 << 22) return hta::report_error(MTFM_HTA_ERR_UNSUPPORTED, "Hq (%d) x head_dim (%d) exceeds 2^22", Hq, d);
     return MTFM_HTA_OK;
 }
 
@@ -465,19 +541,19 @@ Plan plan_backward(int64_t total_kv, int Hq, int Hkv, int d) {
     return p;
 }
 
-template <int D, int G, bool BACK>
+template <int D, int G, int CB, bool BACK>
 hipError_t launch_sweep_as(const Args& a, hipStream_t s) {
     const int64_t members = (int64_t)(BACK ? a.spread : a.ratio) * a.n_pass, groups = (int64_t)a.batch * a.Hkv;
     const int64_t grid = (groups + hta::N_XCD - 1) / hta::N_XCD * hta::N_XCD * members;
-    hipLaunchKernelGGL((sweep_kernel<D, G, BACK>), dim3((unsigned)grid), dim3(D * 4), 0, s, a);
+    hipLaunchKernelGGL((sweep_kernel<D, G, CB, BACK>), dim3((unsigned)grid), dim3(D * 4 / CB), 0, s, a);
     return hipGetLastError();
 }
 template <int D>
 hipError_t launch_sweep_d(const Args& a, bool back, int G, hipStream_t s) {
-    if (!back) return launch_sweep_as<D, 1, false>(a, s);
-    if (G == 1) return launch_sweep_as<D, 1, true>(a, s);
-    if (G == 2) return launch_sweep_as<D, 2, true>(a, s);
-    if constexpr (D < 128) return launch_sweep_as<D, 4, true>(a, s);
+    if (!back) return launch_sweep_as<D, 1, 1, false>(a, s);
+    if (G == 1) return launch_sweep_as<D, 1, 1, true>(a, s);
+    if (G == 2) return launch_sweep_as<D, 2, 1, true>(a, s);
+    if constexpr (D < 128) return launch_sweep_as<D, 4, 1, true>(a, s);
     return hipErrorInvalidValue;
 }
 hipError_t launch_sweep(const Args& a, int d, bool back, int G, hipStream_t s) {
