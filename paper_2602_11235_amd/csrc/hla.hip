@@ -24,29 +24,76 @@ using hta::bf16x4;
 using hta::bf16x8;
 using hta::fast_exp2;
 using hta::floatx4;
-using hta::swizzle;
 
 constexpr int CHUNK = 64;
 constexpr float MIN_LOG2 = -1e4f;  // of a decay: 2^-10000 is 0, and 0 times it is not NaN
 
-struct Pass {
+// A sweep in the tokens' order: the forward pass, or dq
+struct Args {
     const __bf16 *a, *b, *c;
     __bf16* out;
-    float* partial;         // backwards, where a group's heads are spread over workgroups: [spread][total_kv][Hkv][d]
     const float* state_in;  // null: zero
     float* state_out;       // null: not wanted
-    int32_t transposed;     // the state that is read is that of the other sweeps, transposed
-};
-
-struct Args {
-    Pass pass[2];
+    int32_t transposed;     // the state that is read is that of the forward sweep, transposed
     const float* log_decay;
     const int32_t *q_off, *kv_off, *hist_len, *n_targets;
     int64_t total_q, total_kv;
-    int32_t batch, Hq, Hkv, ratio, n_pass, spread;  // spread: workgroups that the heads of a group are dealt to
-    int32_t full;
+    int32_t batch, Hq, Hkv, ratio;
+    int32_t full, max_hist, max_targets;
     float scale;
+    // backwards: dk, dv and the first state's gradient
+    const __bf16 *q, *k, *v, *dout;
+    __bf16 *dk, *dv;
+    float *partial_k, *partial_v;  // where a group's heads are spread over workgroups: [spread][total_kv][Hkv][d] each; null otherwise
+    int32_t spread;
+    // long histories in pieces (seg > 0): `seg` chunks of one kind to a workgroup, at most n_hist pieces of a history and n_tgt of a user's candidates.  The
+    // states in front of the pieces lie in [batch][Hq][n_hist + n_tgt + 1][d][d], in the order of the sweep (backwards the candidates' come first), and the one
+    // behind them all.
+    int32_t seg, n_hist, n_tgt;
+    float *states, *states_back;
 };
+
+// What of a user a workgroup has: chunks [c0, c1) of the sweep, and the index of the state in front of them (-1, without pieces: what the caller gave)
+struct Piece {
+    int c0, c1, state;
+    bool hist;
+};
+__device__ inline int64_t state_index(const Args& g, int u, int h, int i) { return ((int64_t)u * g.Hq + h) * (g.n_hist + g.n_tgt + 1) + i; }
+// Which user, key/value head, piece and member (query head, or set of them) a workgroup has: those that share rows are neighbours on one XCD, and pieces go around
+// the XCDs.  False: none.
+struct Place {
+    int u, kvh, member, piece;
+};
+__device__ inline bool place_of(const Args& g, int members, Place& w) {
+    const int pieces = g.seg ? g.n_hist + g.n_tgt : 1, xcd = blockIdx.x % hta::N_XCD, slot = blockIdx.x / hta::N_XCD;
+    const int64_t unit = (int64_t)(slot / members) * hta::N_XCD + xcd;
+    if (unit >= (int64_t)g.batch * g.Hkv * pieces) return false;
+    const int group = (int)(unit / pieces);
+    w.u = group / g.Hkv, w.kvh = group % g.Hkv, w.member = slot % members, w.piece = (int)(unit % pieces);
+    return true;
+}
+__device__ inline Piece piece_of(const Args& g, int id, int nh, int nt, bool back) {
+    Piece p;
+    if (g.seg == 0) {
+        p.c0 = 0, p.c1 = nh + nt, p.state = -1, p.hist = true;
+        return p;
+    }
+    p.hist = id < g.n_hist;
+    const int n = p.hist ? nh : nt, first = (p.hist ? id : id - g.n_hist) * g.seg, ahead = p.hist == back ? (back ? nt : nh) : 0;
+    p.c0 = ahead + min(first, n), p.c1 = ahead + min(first + g.seg, n);
+    if (back) p.state = p.hist ? (nt + g.seg - 1) / g.seg + id : id - g.n_hist;
+    else p.state = p.hist ? id : (nh + g.seg - 1) / g.seg;
+    return p;
+}
+
+// Tiles in LDS lie in rows of D elements without padding; the 16-byte word w of row r is at position w ^ place<D>(r).  A 16-byte read is served in groups of
+// 16 lanes, 0 .. 3, 12 .. 15 and 20 .. 27 the first (the bank conflicts of two lanes say so), an 8-byte read in groups of 32: with this order neither has a
+// conflict where 16 lanes read a word of 16 rows and the next 16 its neighbour, or a transposing read takes two words of 4 rows and of 4 rows 8 further.
+template <int D>
+__device__ inline int place(int row) {
+    const int h = (row >> 2) & 3, c = (((h ^ (h >> 1)) & 1) << 1) | (h >> 1);
+    return D == 32 ? c : D == 64 ? (((row >> 1) & 1) << 2) | c : ((row & 3) << 2) | c;
+}
 
 __device__ inline floatx4 mfma16(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
@@ -64,7 +111,7 @@ __device__ inline void split8(const float (&x)[8], bf16x8& hi, bf16x8& lo) {
     hi = __builtin_bit_cast(bf16x8, h);
 }
 
-// Where a user's rows lie, whatever the arrays hold: inside the tensors
+// Where a user's rows lie, whatever the arrays hold: inside the tensors, and no more of them than was said
 struct User {
     int64_t q0, kv0;
     int L, T;
@@ -75,360 +122,611 @@ __device__ inline User user_of(const Args& g, int u) {
     r.kv0 = clamp64(g.kv_off[u], 0, g.total_kv);
     r.q0 = clamp64(g.q_off[u], 0, g.total_q);
     const int64_t n_kv = clamp64(g.kv_off[u + 1], r.kv0, g.total_kv) - r.kv0, n_q = clamp64(g.q_off[u + 1], r.q0, g.total_q) - r.q0;
-    r.L = (int)clamp64(g.hist_len[u], 0, g.full ? (n_kv < n_q ? n_kv : n_q) : n_kv);
+    r.L = (int)clamp64(clamp64(g.hist_len[u], 0, g.max_hist), 0, g.full ? (n_kv < n_q ? n_kv : n_q) : n_kv);
     const int64_t left_kv = n_kv - r.L, left_q = g.full ? n_q - r.L : n_q;
-    r.T = (int)clamp64(g.n_targets[u], 0, left_kv < left_q ? left_kv : left_q);
+    r.T = (int)clamp64(clamp64(g.n_targets[u], 0, g.max_targets), 0, left_kv < left_q ? left_kv : left_q);
     return r;
 }
 
-// waves per SIMD that the registers are to leave room for
-constexpr int sweep_waves(int D, int G, int CB) { return D == 32 && G == 1 ? 4 : D * G * CB <= 64 ? 3 : 2; }
-
-// One sweep over a user by a workgroup of D / (16 CB) waves, each with CB blocks of 16 columns.  Forwards a workgroup has one query head, backwards G heads of a group, whose outputs
-// (dv or dk of their common key/value head) it sums.  D[m][n] += A[m][k] B[k][n] of 16x16x32: a lane holds row (column) lane % 16 and k = 8 (lane / 16) ..
-// + 7 of either operand, and column lane % 16, rows 4 (lane / 16) .. + 3 of the result.
-template <int D, int G, int CB, bool BACK>
-__global__ __launch_bounds__(D * 4 / CB, sweep_waves(D, G, CB)) void sweep_kernel(const Args args) {
-    constexpr int NW = D / 16 / CB, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = CHUNK / PART;  // PART: rows that the threads load at a time
-    __shared__ __attribute__((aligned(16))) __bf16 a_s[CHUNK * D], b_s[CHUNK * D], c_s[CHUNK * D], p_s[CHUNK * CHUNK];
-    __shared__ float dots_s[CHUNK];
-    // powers of the heads' decays, as they are and times `scale`: entry ZERO + m holds l^m, m = -64 .. 64, 0 for m < 0
-    constexpr int ZERO = CHUNK, POWERS = 2 * CHUNK + 4;
-    __shared__ float power_s[G][POWERS], scaled_s[G][POWERS];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
-
-    // which user, heads and pass: those that share rows are neighbours on one XCD
-    const int per_pass = BACK ? args.spread : args.ratio, members = per_pass * args.n_pass;
-    const int xcd = blockIdx.x % hta::N_XCD, slot = blockIdx.x / hta::N_XCD;
-    const int group = (slot / members) * hta::N_XCD + xcd, member = slot % members;
-    if (group >= args.batch * args.Hkv) return;
-    const int u = group / args.Hkv, kvh = group % args.Hkv, sub = member % per_pass;
-    const Pass ps = args.pass[member / per_pass];
-    const int qh0 = kvh * args.ratio + sub * G;  // the first of the G query heads
-    const User us = user_of(args, u);
-    const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK, chunks = nh + nt;
-    const bool full = args.full;
-
-    // state: tile t of head g and block b, register v: row 32 (t / 2) + 8 quad + 4 (t % 2) + v, column 16 (CB wave + b) + l16.  (Rows in this order make the accumulators of
-    // two tiles eight consecutive rows: what an operand wants.)
-    floatx4 S[G][CB][2 * KS];
-#pragma unroll
-    for (int g = 0; g < G; g++) {
-        const float* in = ps.state_in ? ps.state_in + ((int64_t)u * args.Hq + qh0 + g) * D * D : nullptr;
-#pragma unroll
-        for (int b = 0; b < CB; b++)
-#pragma unroll
-            for (int t = 0; t < 2 * KS; t++) {
-                const int row = 32 * (t / 2) + 8 * quad + 4 * (t % 2), col = 16 * (CB * wave + b) + l16;
-                S[g][b][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-                if (in) {
-                    if (ps.transposed) S[g][b][t] = *(const floatx4*)(in + col * D + row);
-                    else
-#pragma unroll
-                        for (int v = 0; v < 4; v++) S[g][b][t][v] = in[(row + v) * D + col];
-                }
-            }
+// Bytes from the start of a tile that a lane's reads go to, for rows and words that differ in nothing that place<>() looks at but the bits that are
+// exchanged here.  (Kept out of the compiler's sight in every turn of the loops: it would keep each of the addresses that follow from them in a register.)
+template <int D>
+struct Lane {
+    unsigned stage;  // the word that the thread stages: row tid / (D / 8), word tid % (D / 8)
+    unsigned row;    // word quad of row l16: an operand with its contraction along the row, k = 8 quad ..; words 4 k further by ^ 64 k
+    unsigned tr;     // the first of two transposing reads: rows 8 quad .. + 3, columns 0 .. 15 of the wave's first block
+    unsigned trp;    // the same, columns 8 (l16 & 3) .. + 3: in the order of the state's rows
+    __device__ Lane(int tid, int l16, int quad, int first_block) {
+        const int r = tid / (D / 8), w = tid % (D / 8), t = 8 * quad + (l16 >> 2);
+        stage = r * (D * 2) + ((w ^ place<D>(r)) * 16);
+        row = l16 * (D * 2) + ((quad ^ place<D>(l16)) * 16);
+        tr = t * (D * 2) + (((2 * first_block + ((l16 & 3) >> 1)) ^ place<D>(t)) * 16) + (l16 & 1) * 8;
+        trp = t * (D * 2) + (((l16 & 3) ^ place<D>(t)) * 16);
     }
+    __device__ void forget(int& tid, int& l16, int& quad) { asm volatile("" : "+v"(stage), "+v"(row), "+v"(tr), "+v"(trp), "+v"(tid), "+v"(l16), "+v"(quad)); }
+};
+template <typename T>
+__device__ inline T& lds(char* base, unsigned at) {
+    return *(T*)(base + at);
+}
+// rows r .. r + 3 and r + 4 .. r + 7 of a transposing read at `at` (place<>() of a row 4 further differs by 2 words)
+template <int D>
+__device__ inline bf16x8 read_tr(char* tile, unsigned at) {
+    return hta::lds_read_tr_pair((const __bf16*)(tile + at), (const __bf16*)(tile + (at ^ 32) + 4 * D * 2));
+}
 
-    struct Rows {  // of a chunk: n rows, row r is first + r (backwards through a history: first - r)
-        int64_t q, kv;
-        int n;
-        bool hist;
-    };
-    const auto rows_of = [&](int c) {
-        Rows r;
-        r.hist = BACK ? c >= nt : c < nh;
-        if (r.hist) {
-            const int first = (BACK ? c - nt : c) * CHUNK, at = BACK ? us.L - 1 - first : first;
-            r.n = min(CHUNK, us.L - first);
-            r.kv = us.kv0 + at, r.q = us.q0 + at;
-        } else {
-            const int first = (BACK ? c : c - nh) * CHUNK;
-            r.n = min(CHUNK, us.T - first);
-            r.kv = us.kv0 + us.L + first, r.q = us.q0 + (full ? us.L : 0) + first;
-        }
-        return r;
-    };
-    // A chunk's rows in memory: a uniform address, that of its lowest of 64 rows (backwards through a history row 63, which need not be there), and a
-    // lane's bytes from there
-    const int heads_a = BACK ? args.Hkv : args.Hq, heads_b = BACK ? args.Hq : args.Hkv;
-    const unsigned pitch_a = heads_a * (D * 2), pitch_b = heads_b * (D * 2);
-    const auto lowest = [](bool down, int64_t first) { return down ? first - (CHUNK - 1) : first; };
-    const auto bytes_of = [](bool down, int r, unsigned pitch, int byte) { return __umul24(down ? CHUNK - 1 - r : r, pitch) + byte; };
-
-    // 16-byte words of the three tiles on their way: word tid % C16 of rows tid / C16 + i PART.  Rows that are not there are zero.
-    const int row_t = tid / C16, word_t = tid % C16;
-    bf16x8 av[LOADS], bv[LOADS], cv[LOADS];
-    const auto fetch = [&](int chunk, int g) {
-        const Rows r = rows_of(chunk);
-        const bool asks = full || !r.hist;  // are there query rows?
-        const bool has_a = (BACK || asks) && (G == 1 || g == 0), has_bc = !BACK || asks, down = BACK && r.hist;
-        const int head_a = BACK ? kvh : qh0, head_b = BACK ? qh0 + g : kvh;
-        const int64_t row_b = lowest(down, BACK ? r.q : r.kv) * heads_b + head_b;
-        const char* a = (const char*)(ps.a + (lowest(down, BACK ? r.kv : r.q) * heads_a + head_a) * D);
-        const char *b = (const char*)(ps.b + row_b * D), *c = (const char*)(ps.c + row_b * D);
-#pragma unroll
-        for (int i = 0; i < LOADS; i++) {
-            const int row = row_t + i * PART;
-            const bool there = row < r.n;
-            const unsigned at_a = bytes_of(down, row, pitch_a, word_t * 16), at_b = bytes_of(down, row, pitch_b, word_t * 16);
-            av[i] = bv[i] = cv[i] = bf16x8{};
-            if (there && has_a) av[i] = *(const bf16x8*)(a + at_a);
-            if (there && has_bc) bv[i] = *(const bf16x8*)(b + at_b), cv[i] = *(const bf16x8*)(c + at_b);
-        }
-    };
-    const auto word_at = [](const __bf16* tile, int row, int word) { return tile + row * D + ((word ^ swizzle<D>(row)) * 8); };
-
-    if (chunks > 0) fetch(0, 0);
-    for (int i = tid; i < G * POWERS; i += NT) {
+constexpr int ZERO = CHUNK, POWERS = 2 * CHUNK + 4;  // powers of a decay: entry ZERO + m holds l^m, m = -64 .. 64, 0 for m < 0
+// the tables of `heads` heads from h on, [plain | times scale] each
+template <int NT>
+__device__ inline void fill_powers(float* table, const float* log_decay, int heads, float scale, int tid) {
+    for (int i = tid; i < heads * POWERS; i += NT) {
         const int g = i / POWERS, m = i % POWERS - ZERO;
-        const float g2 = fmaxf(fminf(args.log_decay[qh0 + g], 0.f) * hta::LOG2E, MIN_LOG2);
+        const float g2 = fmaxf(fminf(log_decay[g], 0.f) * hta::LOG2E, MIN_LOG2);
         const float p = m < 0 ? 0.f : fast_exp2(g2 * (float)m);
-        power_s[g][m + ZERO] = p, scaled_s[g][m + ZERO] = p * args.scale;
-    }
-    // (entries of P that a product reads and no chunk writes)
-    for (int i = tid; i < CHUNK * CHUNK / 8; i += NT) ((bf16x8*)p_s)[i] = bf16x8{};
-
-    floatx4 acc[CB][4];
-    for (int c = 0; c < chunks; c++) {
-        const Rows r = rows_of(c);
-        const bool asks = full || !r.hist, down = BACK && r.hist;
-        const bool has_out = BACK || asks, has_bc = !BACK || asks;
-        const bool intra = r.hist && has_out && has_bc, inter = r.hist ? has_out : !BACK, update = r.hist ? has_bc : BACK;
-#pragma unroll
-        for (int g = 0; g < G; g++) {
-            // (the last readers of the tiles are behind the barrier at the end of the turn)
-#pragma unroll
-            for (int i = 0; i < LOADS; i++) {
-                if (g == 0) *(bf16x8*)word_at(a_s, row_t + i * PART, word_t) = av[i];
-                *(bf16x8*)word_at(b_s, row_t + i * PART, word_t) = bv[i];
-                *(bf16x8*)word_at(c_s, row_t + i * PART, word_t) = cv[i];
-            }
-            __syncthreads();
-            if (g + 1 < G) fetch(c, g + 1);
-            else if (c + 1 < chunks) fetch(c + 1, 0);
-
-            if (intra) {
-                // P^T = B A^T with the decays, tiles on and below the diagonal, dealt to the waves
-#pragma unroll
-                for (int t0 = 0; t0 < 10; t0 += NW) {
-                    const int t = t0 + wave;
-                    if (t >= 10) break;
-                    const int it = t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, jt = t - it * (it + 1) / 2;
-                    const int i = 16 * it + l16, j = 16 * jt + 4 * quad;
-                    floatx4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int k = 0; k < KS; k++)
-                        s = mfma16(*(const bf16x8*)word_at(b_s, 16 * jt + l16, 4 * k + quad), *(const bf16x8*)word_at(a_s, i, 4 * k + quad), s);
-                    float w[4];
-                    const float* power = scaled_s[g] + ZERO + i - j;
-#pragma unroll
-                    for (int v = 0; v < 4; v++) w[v] = power[-v];
-                    bf16x4 p;
-#pragma unroll
-                    for (int v = 0; v < 4; v++) {
-                        s[v] *= w[v];
-                        p[v] = (__bf16)(i - j >= v ? s[v] : 0.f);  // (0 times what a later row holds need not be 0)
-                    }
-                    *(bf16x4*)(p_s + i * CHUNK + (((j / 8) ^ swizzle<64>(i)) * 8) + (j & 4)) = p;
-                }
-            } else if (!r.hist) {
-                // own keys only: <a_i, b_i>, NW lanes to a row
-                const int row = tid / NW, part = tid % NW;
-                float dot = 0.f;
-#pragma unroll
-                for (int k = 0; k < C16 / NW; k++)
-                    dot = hta::dot_bf16x8(dot, *(const bf16x8*)word_at(a_s, row, C16 / NW * part + k), *(const bf16x8*)word_at(b_s, row, C16 / NW * part + k));
-                dot = hta::sum_lanes<NW>(dot);
-                if (part == 0) dots_s[row] = dot * args.scale;
-            }
-            // o^T = S^T A^T, row i of it times l^(i+1) scale (candidates: l scale, backwards: l^i)
-            floatx4 o[CB][4];
-            if (inter) {
-                bf16x8 s[CB][KS];
-#pragma unroll
-                for (int b = 0; b < CB; b++)
-#pragma unroll
-                    for (int k = 0; k < KS; k++)
-#pragma unroll
-                        for (int v = 0; v < 4; v++) s[b][k][v] = (__bf16)S[g][b][2 * k][v], s[b][k][4 + v] = (__bf16)S[g][b][2 * k + 1][v];
-#pragma unroll
-                for (int it = 0; it < 4; it++)
-#pragma unroll
-                    for (int k = 0; k < KS; k++) {
-                        const bf16x8 a = *(const bf16x8*)word_at(a_s, 16 * it + l16, 4 * k + quad);
-#pragma unroll
-                        for (int b = 0; b < CB; b++) o[b][it] = mfma16(s[b][k], a, k == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : o[b][it]);
-                    }
-            }
-            __syncthreads();
-            // C^T: this wave's columns of c, rows 32 k + 8 quad .. + 7
-            bf16x8 ct[CB][2];
-#pragma unroll
-            for (int b = 0; b < CB; b++)
-#pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    const int row = 32 * k + 8 * quad + (l16 >> 2), word = 2 * (CB * wave + b) + ((l16 & 3) >> 1), off = (l16 & 1) * 4;
-                    ct[b][k] = hta::lds_read_tr_pair(word_at(c_s, row, word) + off, word_at(c_s, row + 4, word) + off);
-                }
-            floatx4 within[CB][4];
-#pragma unroll
-            for (int b = 0; b < CB; b++)
-#pragma unroll
-                for (int it = 0; it < 4; it++) within[b][it] = floatx4{0.f, 0.f, 0.f, 0.f};
-            if (intra) {
-#pragma unroll
-                for (int it = 0; it < 4; it++)
-#pragma unroll
-                    for (int k = 0; k <= it / 2; k++) {
-                        const int i = 16 * it + l16;
-                        const bf16x8 p = *(const bf16x8*)(p_s + i * CHUNK + (((4 * k + quad) ^ swizzle<64>(i)) * 8));
-#pragma unroll
-                        for (int b = 0; b < CB; b++) within[b][it] = mfma16(ct[b][k], p, within[b][it]);
-                    }
-                // An infinity or a NaN in c reaches the rows in front of it as 0 times itself, and the last rows in any case: then row by row.
-                float zero = 0.f;
-#pragma unroll
-                for (int b = 0; b < CB; b++)
-#pragma unroll
-                    for (int v = 0; v < 4; v++) zero = fmaf(within[b][3][v], 0.f, zero);
-                if (__ballot(zero != zero) != 0) {
-#pragma unroll
-                    for (int b = 0; b < CB; b++)
-#pragma unroll
-                        for (int it = 0; it < 4; it++) within[b][it] = floatx4{0.f, 0.f, 0.f, 0.f};
-                    for (int j = 0; j < CHUNK; j++) {
-#pragma unroll
-                        for (int b = 0; b < CB; b++) {
-                            const bf16x4 cj = *(const bf16x4*)(word_at(c_s, j, 2 * (CB * wave + b) + (quad >> 1)) + (quad & 1) * 4);
-#pragma unroll
-                            for (int it = 0; it < 4; it++) {
-                                const int i = 16 * it + l16;
-                                const float p = (float)p_s[i * CHUNK + (((j / 8) ^ swizzle<64>(i)) * 8) + (j & 7)];
-#pragma unroll
-                                for (int v = 0; v < 4; v++) within[b][it][v] += j <= i ? p * (float)cj[v] : 0.f;
-                            }
-                        }
-                    }
-                }
-            } else if (!r.hist) {
-#pragma unroll
-                for (int b = 0; b < CB; b++)
-#pragma unroll
-                    for (int it = 0; it < 4; it++) {
-                        const int i = 16 * it + l16;
-                        const bf16x4 ci = *(const bf16x4*)(word_at(c_s, i, 2 * (CB * wave + b) + (quad >> 1)) + (quad & 1) * 4);
-#pragma unroll
-                        for (int v = 0; v < 4; v++) within[b][it][v] = dots_s[i] * (float)ci[v];
-                    }
-            }
-            if (inter) {
-                const float* power = r.hist ? (BACK ? power_s[g] + ZERO : scaled_s[g] + ZERO + 1) + l16 : scaled_s[g] + ZERO + 1;
-                const int step = r.hist ? 16 : 0;
-#pragma unroll
-                for (int it = 0; it < 4; it++) {
-                    const float f = power[it * step];
-#pragma unroll
-                    for (int b = 0; b < CB; b++)
-#pragma unroll
-                        for (int v = 0; v < 4; v++) within[b][it][v] = fmaf(o[b][it][v], f, within[b][it][v]);
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < CB; b++)
-#pragma unroll
-                for (int it = 0; it < 4; it++) acc[b][it] = g == 0 ? within[b][it] : acc[b][it] + within[b][it];
-            if (has_out && g == G - 1) {
-                const int64_t base = (lowest(down, BACK ? r.kv : r.q) * heads_a + (BACK ? kvh : qh0)) * D;
-                char* out = (char*)(ps.out + base);
-                char* partial = (char*)(ps.partial + (int64_t)sub * args.total_kv * args.Hkv * D + base);
-#pragma unroll
-                for (int it = 0; it < 4; it++) {
-                    if (16 * it + l16 < r.n) {
-                        const unsigned at = bytes_of(down, 16 * it + l16, pitch_a, (16 * CB * wave + 4 * quad) * 2);
-#pragma unroll
-                        for (int b = 0; b < CB; b++) {
-                            if (BACK && ps.partial) {
-                                *(floatx4*)(partial + 2 * at + 64 * b) = acc[b][it];
-                            } else {
-                                bf16x4 x;
-#pragma unroll
-                                for (int v = 0; v < 4; v++) x[v] = (__bf16)acc[b][it][v];
-                                *(bf16x4*)(out + at + 32 * b) = x;
-                            }
-                        }
-                    }
-                }
-            }
-            // the state behind the chunk: l^n S + B^T (w c), where w c goes in two halves of 8 bits each, so that float32 keeps 16 of it
-            if (r.hist) {
-                const float keep = power_s[g][ZERO + r.n];
-#pragma unroll
-                for (int b = 0; b < CB; b++)
-#pragma unroll
-                    for (int t = 0; t < 2 * KS; t++) S[g][b][t] *= keep;
-            }
-            if (update) {
-#pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    bf16x8 hi[CB], lo[CB];
-                    float w[8];
-                    // l^(n-1-j) (backwards l^(n-j) scale); rows that are not there are zero, and so are these behind the table's end
-                    const float* p = (BACK ? scaled_s[g] + ZERO + r.n : power_s[g] + ZERO + r.n - 1) - (32 * k + 8 * quad);
-#pragma unroll
-                    for (int e = 0; e < 8; e++) w[e] = r.hist ? p[-e] : scaled_s[g][ZERO + 1];
-#pragma unroll
-                    for (int b = 0; b < CB; b++) {
-                        float x[8];
-#pragma unroll
-                        for (int e = 0; e < 8; e++) x[e] = w[e] * (float)ct[b][k][e];
-                        split8(x, hi[b], lo[b]);
-                    }
-#pragma unroll
-                    for (int t = 0; t < 2 * KS; t++) {
-                        const int row = 32 * k + 8 * quad + (l16 >> 2), word = 4 * (t / 2) + (l16 & 3), off = 4 * (t % 2);
-                        const bf16x8 bt = hta::lds_read_tr_pair(word_at(b_s, row, word) + off, word_at(b_s, row + 4, word) + off);
-#pragma unroll
-                        for (int b = 0; b < CB; b++) {
-                            S[g][b][t] = mfma16(bt, hi[b], S[g][b][t]);
-                            S[g][b][t] = mfma16(bt, lo[b], S[g][b][t]);
-                        }
-                    }
-                }
-            }
-            __syncthreads();
-        }
-    }
-    if (ps.state_out) {
-#pragma unroll
-        for (int g = 0; g < G; g++) {
-            float* out = ps.state_out + ((int64_t)u * args.Hq + qh0 + g) * D * D;
-#pragma unroll
-            for (int b = 0; b < CB; b++)
-#pragma unroll
-                for (int t = 0; t < 2 * KS; t++)
-#pragma unroll
-                    for (int v = 0; v < 4; v++) out[(32 * (t / 2) + 8 * quad + 4 * (t % 2) + v) * D + 16 * (CB * wave + b) + l16] = S[g][b][t][v];
-        }
+        table[2 * g * POWERS + m + ZERO] = p, table[(2 * g + 1) * POWERS + m + ZERO] = p * scale;
     }
 }
 
+// One tile of P^T = B A^T with the decays, rows i = 16 it .. of A (queries), rows j = 16 jt .. of B, to P[i][j]
+template <int D>
+__device__ inline void score_tile(char* a, char* b, char* p_tile, const float* scaled, const Lane<D>& at, const Lane<CHUNK>& at_p, int it, int jt, int l16, int quad) {
+    floatx4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < D / 32; k++)
+        s = mfma16(lds<bf16x8>(b + jt * (16 * D * 2), at.row ^ (64 * k)), lds<bf16x8>(a + it * (16 * D * 2), at.row ^ (64 * k)), s);
+    const int d = 16 * (it - jt) + l16 - 4 * quad;  // i - j
+    const float* power = scaled + ZERO + d;
+    float w[4];
+#pragma unroll
+    for (int v = 0; v < 4; v++) w[v] = power[-v];
+    bf16x4 p;
+#pragma unroll
+    for (int v = 0; v < 4; v++) {
+        s[v] *= w[v];
+        p[v] = (__bf16)(d >= v ? s[v] : 0.f);  // (0 times what a later row holds need not be 0)
+    }
+    // word 2 jt + quad / 2 of row i, its half quad % 2: from word quad
+    const unsigned to = (at_p.row ^ ((quad ^ (quad >> 1)) * 16) ^ (32 * jt)) + (quad & 1) * 8;
+    lds<bf16x4>(p_tile + it * (16 * CHUNK * 2), to) = p;
+}
+__device__ inline int tile_row(int t) { return t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0; }  // of the ten tiles on and below the diagonal
+
+// C^T P^T for rows 16 it .. of a chunk: what its own rows add.  `odd`: an infinity or a NaN in c reaches all rows as 0 times itself, the last ones in any case
+// (so they come first); then it is done row by row.
+template <int D, int IT>
+__device__ inline floatx4 within_chunk(const bf16x8 (&ct)[2], char* p_tile, char* c_tile, const Lane<CHUNK>& at_p, int block, bool& odd, int l16, int quad) {
+    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k <= IT / 2; k++) x = mfma16(ct[k], lds<bf16x8>(p_tile + IT * (16 * CHUNK * 2), at_p.row ^ (64 * k)), x);
+    if (IT == 3) {
+        const float zero = fmaf(x[0], 0.f, x[1] * 0.f) + fmaf(x[2], 0.f, x[3] * 0.f);
+        odd = __ballot(zero != zero) != 0;
+    }
+    if (odd) {
+        const int i = 16 * IT + l16;
+        x = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < 16 * IT + 16; j++) {
+            const float p = (float)lds<__bf16>(p_tile, i * (CHUNK * 2) + (((j / 8) ^ place<CHUNK>(i)) * 16) + (j & 7) * 2);
+            const bf16x4 c = lds<bf16x4>(c_tile, j * (D * 2) + (((2 * block + (quad >> 1)) ^ place<D>(j)) * 16) + (quad & 1) * 8);
+#pragma unroll
+            for (int v = 0; v < 4; v++) x[v] += j <= i ? p * (float)c[v] : 0.f;
+        }
+    }
+    return x;
+}
+
+// candidates: <a_i, b_i> scale to dots[i], NT / 64 lanes to a row
+template <int D, int NT>
+__device__ inline void own_dots(char* a, char* b, float* dots, float scale, int tid) {
+    constexpr int LANES = NT / CHUNK, WORDS = D / 8 / LANES;
+    const int row = tid / LANES, part = tid % LANES;
+    float dot = 0.f;
+#pragma unroll
+    for (int k = 0; k < WORDS; k++) {
+        const unsigned at = row * (D * 2) + (((WORDS * part + k) ^ place<D>(row)) * 16);
+        dot = hta::dot_bf16x8(dot, lds<bf16x8>(a, at), lds<bf16x8>(b, at));
+    }
+    dot = hta::sum_lanes<LANES>(dot);
+    if (part == 0) dots[row] = dot * scale;
+}
+template <int D>
+__device__ inline floatx4 own_term(const float* dots, char* c_tile, int block, int i, int quad) {
+    const bf16x4 c = lds<bf16x4>(c_tile, i * (D * 2) + (((2 * block + (quad >> 1)) ^ place<D>(i)) * 16) + (quad & 1) * 8);
+    const float dot = dots[i];
+    return floatx4{dot * (float)c[0], dot * (float)c[1], dot * (float)c[2], dot * (float)c[3]};
+}
+
+// A state's columns, 16 to a wave (block `block`): tile t, register v of a lane: row 32 (t / 2) + 8 quad + 4 (t % 2) + v, column 16 block + l16.  (Rows in this
+// order make the accumulators of two tiles eight consecutive rows: what an operand wants.)
+template <int D>
+struct State {
+    static constexpr int TILES = D / 16, KS = D / 32;
+    floatx4 t[TILES];
+    __device__ static int row(int tile, int quad) { return 32 * (tile / 2) + 8 * quad + 4 * (tile % 2); }
+    __device__ void zero() {
+#pragma unroll
+        for (int i = 0; i < TILES; i++) t[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ void load(const float* in, bool transposed, int block, int l16, int quad) {
+        const int col = 16 * block + l16;
+#pragma unroll
+        for (int i = 0; i < TILES; i++) {
+            if (transposed) t[i] = *(const floatx4*)(in + col * D + row(i, quad));
+            else
+#pragma unroll
+                for (int v = 0; v < 4; v++) t[i][v] = in[(row(i, quad) + v) * D + col];
+        }
+    }
+    __device__ void store(float* out, int block, int l16, int quad) const {
+        const int col = 16 * block + l16;
+#pragma unroll
+        for (int i = 0; i < TILES; i++)
+#pragma unroll
+            for (int v = 0; v < 4; v++) out[(row(i, quad) + v) * D + col] = t[i][v];
+    }
+    __device__ void keep(float f) {
+#pragma unroll
+        for (int i = 0; i < TILES; i++) t[i] *= f;
+    }
+    __device__ void rounded(bf16x8 (&s)[KS]) const {  // operands: rows 32 k + 8 quad .. + 7
+#pragma unroll
+        for (int k = 0; k < KS; k++)
+#pragma unroll
+            for (int v = 0; v < 4; v++) s[k][v] = (__bf16)t[2 * k][v], s[k][4 + v] = (__bf16)t[2 * k + 1][v];
+    }
+    // += B^T (w c): w c goes in as two bf16 values, so that float32 keeps 16 bits of it.  w[-j]: the weight of row j (rows that are not there are zero,
+    // and so are the weights behind the table's end); step 0: the same for all.
+    __device__ void add(char* b_tile, const bf16x8 (&ct)[2], const float* w, int step, const Lane<D>& at, int quad) {
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const float* p = w - step * (32 * k + 8 * quad);
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[e] = p[-e * step] * (float)ct[k][e];
+            bf16x8 hi, lo;
+            split8(x, hi, lo);
+#pragma unroll
+            for (int i = 0; i < TILES; i++) {
+                const bf16x8 bt = read_tr<D>(b_tile + 32 * k * (D * 2) + 8 * (i % 2), at.trp ^ (64 * (i / 2)));
+                t[i] = mfma16(bt, hi, t[i]);
+                t[i] = mfma16(bt, lo, t[i]);
+            }
+        }
+    }
+};
+
+// A chunk's rows in memory: a uniform address, that of the lowest of 64 rows (backwards through a history row 63, which need not be there), and a lane's
+// bytes from there
+__device__ inline int64_t lowest(bool down, int64_t first) { return down ? first - (CHUNK - 1) : first; }
+__device__ inline unsigned bytes_of(bool down, int r, unsigned pitch, int byte) { return __umul24(down ? CHUNK - 1 - r : r, pitch) + byte; }
+
+struct Rows {  // of a chunk: n rows, row r is first + r (backwards through a history: first - r)
+    int64_t q, kv;
+    int n;
+    bool hist;
+};
+
+// One sweep over a user's head in the tokens' order by a workgroup of D / 16 waves, each with 16 of the state's columns.  D[m][n] += A[m][k] B[k][n] of
+// 16x16x32: a lane holds row (column) lane % 16 and k = 8 (lane / 16) .. + 7 of either operand, and column lane % 16, rows 4 (lane / 16) .. + 3 of the result.
+template <int D>
+__global__ __launch_bounds__(D * 4, D == 128 ? 2 : 4) void sweep_kernel(const Args args) {
+    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = CHUNK / PART, TILE = CHUNK * D * 2;
+    __shared__ __attribute__((aligned(16))) char a_s[TILE], b_s[TILE], c_s[TILE], p_s[CHUNK * CHUNK * 2];
+    __shared__ float dots_s[CHUNK], powers_s[2 * POWERS];
+    int tid = threadIdx.x, l16 = tid & 15, quad = (tid >> 4) & 3;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    Place place;
+    if (!place_of(args, args.ratio, place)) return;
+    const int u = place.u, kvh = place.kvh, qh = kvh * args.ratio + place.member;
+    const User us = user_of(args, u);
+    const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK;
+    const bool full = args.full;
+    const Piece piece = piece_of(args, place.piece, nh, nt, false);
+    if (args.seg && (piece.c0 >= piece.c1 || (piece.hist && !full))) return;
+
+    State<D> S;
+    if (piece.state >= 0) S.load(args.states + state_index(args, u, qh, piece.state) * D * D, false, wave, l16, quad);
+    else if (args.state_in) S.load(args.state_in + ((int64_t)u * args.Hq + qh) * D * D, args.transposed, wave, l16, quad);
+    else S.zero();
+
+    const auto rows_of = [&](int c) {
+        Rows r;
+        r.hist = c < nh;
+        const int first = (r.hist ? c : c - nh) * CHUNK;
+        r.n = min(CHUNK, (r.hist ? us.L : us.T) - first);
+        r.kv = us.kv0 + (r.hist ? 0 : us.L) + first, r.q = us.q0 + (!r.hist && full ? us.L : 0) + first;
+        return r;
+    };
+    // 16-byte words of the three tiles on their way: word tid % C16 of rows tid / C16 + i PART.  Rows that are not there are zero.
+    const unsigned pitch_q = args.Hq * (D * 2), pitch_kv = args.Hkv * (D * 2);
+    bf16x8 av[LOADS], bv[LOADS], cv[LOADS];
+    const auto fetch = [&](int chunk) {
+        const Rows r = rows_of(chunk);
+        const bool asks = full || !r.hist;
+        const char* a = (const char*)(args.a + (r.q * args.Hq + qh) * D);
+        const char *b = (const char*)(args.b + (r.kv * args.Hkv + kvh) * D), *c = (const char*)(args.c + (r.kv * args.Hkv + kvh) * D);
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int row = tid / C16 + i * PART;
+            const unsigned at_a = bytes_of(false, row, pitch_q, tid % C16 * 16), at_b = bytes_of(false, row, pitch_kv, tid % C16 * 16);
+            av[i] = bv[i] = cv[i] = bf16x8{};
+            if (row < r.n) {
+                if (asks) av[i] = *(const bf16x8*)(a + at_a);
+                bv[i] = *(const bf16x8*)(b + at_b), cv[i] = *(const bf16x8*)(c + at_b);
+            }
+        }
+    };
+
+    if (piece.c0 < piece.c1) fetch(piece.c0);
+    fill_powers<NT>(powers_s, args.log_decay + qh, 1, args.scale, tid);
+    const float *power = powers_s, *scaled = powers_s + POWERS;
+    // (entries of P that a product reads and no chunk writes)
+    for (int i = tid; i < CHUNK * CHUNK / 8; i += NT) ((bf16x8*)p_s)[i] = bf16x8{};
+    Lane<D> at(tid, l16, quad, wave);
+    Lane<CHUNK> at_p(0, l16, quad, 0);
+
+    for (int c = piece.c0; c < piece.c1; c++) {
+        const Rows r = rows_of(c);
+        const bool asks = full || !r.hist;
+        at.forget(tid, l16, quad);
+        at_p.forget(tid, l16, quad);
+        // (the last readers of the tiles are behind the barrier at the end of the turn)
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            lds<bf16x8>(a_s + i * PART * (D * 2), at.stage) = av[i];
+            lds<bf16x8>(b_s + i * PART * (D * 2), at.stage) = bv[i];
+            lds<bf16x8>(c_s + i * PART * (D * 2), at.stage) = cv[i];
+        }
+        __syncthreads();
+        if (c + 1 < piece.c1) fetch(c + 1);
+        if (r.hist && asks) {
+#pragma unroll
+            for (int t0 = 0; t0 < 10; t0 += NW) {
+                const int t = t0 + wave, it = tile_row(t), jt = t - it * (it + 1) / 2;
+                if (t < 10) score_tile<D>(a_s, b_s, p_s, scaled, at, at_p, it, jt, l16, quad);
+            }
+        } else if (!r.hist) {
+            own_dots<D, NT>(a_s, b_s, dots_s, args.scale, tid);
+        }
+        // o^T = S^T A^T, row i of it times l^(i+1) scale (candidates: l scale)
+        floatx4 o[4];
+        if (asks) {
+            bf16x8 s[KS];
+            S.rounded(s);
+#pragma unroll
+            for (int it = 0; it < 4; it++)
+#pragma unroll
+                for (int k = 0; k < KS; k++)
+                    o[it] = mfma16(s[k], lds<bf16x8>(a_s + it * (16 * D * 2), at.row ^ (64 * k)), k == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : o[it]);
+        }
+        __syncthreads();
+        bf16x8 ct[2];  // C^T: this wave's columns of c, rows 32 k + 8 quad .. + 7
+#pragma unroll
+        for (int k = 0; k < 2; k++) ct[k] = read_tr<D>(c_s + 32 * k * (D * 2), at.tr);
+        if (asks) {
+            char* out = (char*)(args.out + (r.q * args.Hq + qh) * D);
+            const float* f = scaled + ZERO + 1 + (r.hist ? l16 : 0);
+            const int step = r.hist ? 16 : 0;
+            bool odd = false;
+            hta::static_for<0, 4>([&](auto I) {
+                constexpr int it = 3 - decltype(I)::value;
+                const int i = 16 * it + l16;
+                const floatx4 x = r.hist ? within_chunk<D, it>(ct, p_s, c_s, at_p, wave, odd, l16, quad) : own_term<D>(dots_s, c_s, wave, i, quad);
+                const float w = f[it * step];
+                bf16x4 y;
+#pragma unroll
+                for (int v = 0; v < 4; v++) y[v] = (__bf16)fmaf(o[it][v], w, x[v]);
+                if (i < r.n) *(bf16x4*)(out + bytes_of(false, i, pitch_q, 32 * wave + 8 * quad)) = y;
+            });
+        }
+        if (r.hist) {  // the state behind the chunk: l^n S + B^T (w c), w_j = l^(n-1-j)
+            S.keep(power[ZERO + r.n]);
+            S.add(b_s, ct, power + ZERO + r.n - 1, 1, at, quad);
+        }
+        __syncthreads();
+    }
+    if (args.state_out && !args.seg) S.store(args.state_out + ((int64_t)u * args.Hq + qh) * D * D, wave, l16, quad);
+}
+
+// dk, dv and the first state's gradient: a sweep from a user's candidates over its history's end to its beginning, for G query heads of a group, whose
+// gradients it sums.  With R the state's gradient, rows in the sweep's order, i, j counted from a chunk's start and R handed on decayed already,
+//   dv_i = l^i k_i R + scale sum_(j<=i) l^(i-j) <k_i, q_j> dout_j,     dk_i = l^i v_i R^T + scale sum_(j<=i) l^(i-j) <v_i, dout_j> q_j,
+//   R <- l^n R + scale sum_j l^(n-j) q_j dout_j^T.
+// A wave owns 16 columns of R, and the same columns of dv and of dk; R^T, which the latter needs, is R rounded in LDS, read transposed.
+template <int D, int G>
+__global__ __launch_bounds__(D * 4, 2) void back_kernel(const Args args) {
+    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = CHUNK / PART, TILE = CHUNK * D * 2;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    char *k_s = smem, *v_s = k_s + TILE, *q_s = v_s + TILE, *g_s = q_s + TILE, *pq_s = g_s + TILE, *pg_s = pq_s + CHUNK * CHUNK * 2, *r_s = pg_s + CHUNK * CHUNK * 2;
+    float *dots_q = (float*)(r_s + D * D * 2), *dots_g = dots_q + CHUNK, *powers_s = dots_g + CHUNK;
+    int tid = threadIdx.x, l16 = tid & 15, quad = (tid >> 4) & 3;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    Place place;
+    if (!place_of(args, args.spread, place)) return;
+    const int u = place.u, kvh = place.kvh, sub = place.member, qh0 = kvh * args.ratio + sub * G;
+    const User us = user_of(args, u);
+    const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK;
+    const bool full = args.full;
+    const Piece piece = piece_of(args, place.piece, nh, nt, true);
+    if (args.seg && piece.c0 >= piece.c1) return;
+
+    State<D> R[G];
+#pragma unroll
+    for (int g = 0; g < G; g++) {
+        if (piece.state >= 0) R[g].load(args.states_back + state_index(args, u, qh0 + g, piece.state) * D * D, false, wave, l16, quad);
+        else if (args.state_in) R[g].load(args.state_in + ((int64_t)u * args.Hq + qh0 + g) * D * D, false, wave, l16, quad);
+        else R[g].zero();
+    }
+    const auto rows_of = [&](int c) {
+        Rows r;
+        r.hist = c >= nt;
+        const int first = (r.hist ? c - nt : c) * CHUNK, at = r.hist ? us.L - 1 - first : us.L + first;
+        r.n = min(CHUNK, (r.hist ? us.L : us.T) - first);
+        r.kv = us.kv0 + at, r.q = us.q0 + (full ? at : first);  // (q of a history's rows: only where they ask)
+        return r;
+    };
+    const unsigned pitch_q = args.Hq * (D * 2), pitch_kv = args.Hkv * (D * 2);
+    bf16x8 kw[LOADS], vw[LOADS], qw[LOADS], gw[LOADS];
+    const auto fetch_kv = [&](int chunk) {
+        const Rows r = rows_of(chunk);
+        const int64_t first = (lowest(r.hist, r.kv) * args.Hkv + kvh) * D;
+        const char *k = (const char*)(args.k + first), *v = (const char*)(args.v + first);
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int row = tid / C16 + i * PART;
+            const unsigned at = bytes_of(r.hist, row, pitch_kv, tid % C16 * 16);
+            kw[i] = vw[i] = bf16x8{};
+            if (row < r.n) kw[i] = *(const bf16x8*)(k + at), vw[i] = *(const bf16x8*)(v + at);
+        }
+    };
+    const auto fetch_q = [&](int chunk, int g) {
+        const Rows r = rows_of(chunk);
+        const int64_t first = (lowest(r.hist, r.q) * args.Hq + qh0 + g) * D;
+        const char *q = (const char*)(args.q + first), *dout = (const char*)(args.dout + first);
+        const bool asks = full || !r.hist;
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int row = tid / C16 + i * PART;
+            const unsigned at = bytes_of(r.hist, row, pitch_q, tid % C16 * 16);
+            qw[i] = gw[i] = bf16x8{};
+            if (row < r.n && asks) qw[i] = *(const bf16x8*)(q + at), gw[i] = *(const bf16x8*)(dout + at);
+        }
+    };
+    if (piece.c0 < piece.c1) fetch_kv(piece.c0), fetch_q(piece.c0, 0);
+    fill_powers<NT>(powers_s, args.log_decay + qh0, G, args.scale, tid);
+    for (int i = tid; i < 2 * CHUNK * CHUNK / 8; i += NT) lds<bf16x8>(pq_s, i * 16) = bf16x8{};
+    Lane<D> at(tid, l16, quad, wave);
+    Lane<CHUNK> at_p(0, l16, quad, 0);
+
+    floatx4 acc_v[4], acc_k[4];
+    for (int c = piece.c0; c < piece.c1; c++) {
+        const Rows r = rows_of(c);
+        const bool asks = full || !r.hist;
+#pragma unroll
+        for (int g = 0; g < G; g++) {
+            const float *power = powers_s + 2 * g * POWERS, *scaled = power + POWERS;
+            at.forget(tid, l16, quad);
+            at_p.forget(tid, l16, quad);
+#pragma unroll
+            for (int i = 0; i < LOADS; i++) {
+                if (g == 0) {
+                    lds<bf16x8>(k_s + i * PART * (D * 2), at.stage) = kw[i];
+                    lds<bf16x8>(v_s + i * PART * (D * 2), at.stage) = vw[i];
+                }
+                lds<bf16x8>(q_s + i * PART * (D * 2), at.stage) = qw[i];
+                lds<bf16x8>(g_s + i * PART * (D * 2), at.stage) = gw[i];
+            }
+            bf16x8 s[KS];
+            if (r.hist) {  // R^T for the other waves: row 16 wave + l16 of it, 32 k + 8 quad .. + 7
+                R[g].rounded(s);
+#pragma unroll
+                for (int k = 0; k < KS; k++) lds<bf16x8>(r_s + wave * (16 * D * 2), at.row ^ (64 * k)) = s[k];
+            }
+            __syncthreads();
+            if (g + 1 < G) fetch_q(c, g + 1);
+            else if (c + 1 < piece.c1) fetch_q(c + 1, 0);
+            if (g == G - 1 && c + 1 < piece.c1) fetch_kv(c + 1);
+
+            if (r.hist && asks) {
+#pragma unroll
+                for (int t0 = 0; t0 < 20; t0 += NW) {
+                    const int t = t0 + wave, tt = t >= 10 ? t - 10 : t, it = tile_row(tt), jt = tt - it * (it + 1) / 2;
+                    if (t < 20) score_tile<D>(t >= 10 ? v_s : k_s, t >= 10 ? g_s : q_s, t >= 10 ? pg_s : pq_s, scaled, at, at_p, it, jt, l16, quad);
+                }
+            } else if (!r.hist) {
+                own_dots<D, NT>(k_s, q_s, dots_q, args.scale, tid);
+                own_dots<D, NT>(v_s, g_s, dots_g, args.scale, tid);
+            }
+            __syncthreads();
+            bf16x8 gt[2], qt[2];  // this wave's columns of dout and q, rows 32 k + 8 quad .. + 7
+#pragma unroll
+            for (int k = 0; k < 2; k++) gt[k] = read_tr<D>(g_s + 32 * k * (D * 2), at.tr), qt[k] = read_tr<D>(q_s + 32 * k * (D * 2), at.tr);
+            bool odd_g = false, odd_q = false;
+            hta::static_for<0, 4>([&](auto I) {
+                constexpr int it = 3 - decltype(I)::value;
+                const int i = 16 * it + l16;
+                floatx4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+                if (!r.hist) {
+                    x = own_term<D>(dots_q, g_s, wave, i, quad), y = own_term<D>(dots_g, q_s, wave, i, quad);
+                } else {
+                    if (asks) {
+                        x = within_chunk<D, it>(gt, pq_s, g_s, at_p, wave, odd_g, l16, quad);
+                        y = within_chunk<D, it>(qt, pg_s, q_s, at_p, wave, odd_q, l16, quad);
+                    }
+                    floatx4 o = {0.f, 0.f, 0.f, 0.f}, p = o;
+#pragma unroll
+                    for (int k = 0; k < KS; k++) {
+                        o = mfma16(s[k], lds<bf16x8>(k_s + it * (16 * D * 2), at.row ^ (64 * k)), o);
+                        p = mfma16(read_tr<D>(r_s + 32 * k * (D * 2), at.tr), lds<bf16x8>(v_s + it * (16 * D * 2), at.row ^ (64 * k)), p);
+                    }
+                    const float f = power[ZERO + i];
+#pragma unroll
+                    for (int v = 0; v < 4; v++) x[v] = fmaf(o[v], f, x[v]), y[v] = fmaf(p[v], f, y[v]);
+                }
+                acc_v[it] = g == 0 ? x : acc_v[it] + x;
+                acc_k[it] = g == 0 ? y : acc_k[it] + y;
+            });
+            if (g == G - 1) {
+                const int64_t base = (lowest(r.hist, r.kv) * args.Hkv + kvh) * D, slab = (int64_t)sub * args.total_kv * args.Hkv * D;
+#pragma unroll
+                for (int it = 0; it < 4; it++) {
+                    const int i = 16 * it + l16;
+                    if (i >= r.n) continue;
+                    const unsigned to = bytes_of(r.hist, i, pitch_kv, 32 * wave + 8 * quad);
+                    if (args.partial_k) {
+                        *(floatx4*)((char*)(args.partial_v + slab + base) + 2 * to) = acc_v[it];
+                        *(floatx4*)((char*)(args.partial_k + slab + base) + 2 * to) = acc_k[it];
+                    } else {
+                        bf16x4 x, y;
+#pragma unroll
+                        for (int v = 0; v < 4; v++) x[v] = (__bf16)acc_v[it][v], y[v] = (__bf16)acc_k[it][v];
+                        *(bf16x4*)((char*)(args.dv + base) + to) = x;
+                        *(bf16x4*)((char*)(args.dk + base) + to) = y;
+                    }
+                }
+            }
+            if (r.hist) R[g].keep(power[ZERO + r.n]);
+            if (asks) R[g].add(q_s, gt, scaled + ZERO + (r.hist ? r.n : 1), r.hist ? 1 : 0, at, quad);
+            __syncthreads();
+        }
+    }
+    if (args.state_out && !args.seg)
+#pragma unroll
+        for (int g = 0; g < G; g++) R[g].store(args.state_out + ((int64_t)u * args.Hq + qh0 + g) * D * D, wave, l16, quad);
+}
+template <int D, int G>
+constexpr int back_lds() { return 4 * CHUNK * D * 2 + 2 * CHUNK * CHUNK * 2 + D * D * 2 + (2 * CHUNK + 2 * G * POWERS) * 4; }
+
+// What each piece adds to a state that starts at zero: forwards sum_j l^(n-1-j) b_j c_j^T over a history's piece, backwards scale times sum_j l^(n-j) q_j dout_j^T
+// over either kind (candidates: l).  blockIdx.y: 1 backwards.
+template <int D>
+__global__ __launch_bounds__(D * 4, 4) void states_kernel(const Args args, int first_job) {
+    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, PART = NT / C16, LOADS = CHUNK / PART, TILE = CHUNK * D * 2;
+    __shared__ __attribute__((aligned(16))) char b_s[TILE], c_s[TILE];
+    __shared__ float powers_s[2 * POWERS];
+    int tid = threadIdx.x, l16 = tid & 15, quad = (tid >> 4) & 3;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool back = (int)blockIdx.y + first_job == 1;
+
+    Place place;
+    if (!place_of(args, args.ratio, place)) return;
+    const int u = place.u, kvh = place.kvh, qh = kvh * args.ratio + place.member;
+    const User us = user_of(args, u);
+    const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK;
+    const Piece piece = piece_of(args, place.piece, nh, nt, back);
+    if (piece.c0 >= piece.c1 || (back ? piece.hist && !args.full : !piece.hist)) return;
+
+    const int heads = back ? args.Hq : args.Hkv, head = back ? qh : kvh;
+    const unsigned pitch = heads * (D * 2);
+    const __bf16 *bg = back ? args.q : args.b, *cg = back ? args.dout : args.c;
+    bf16x8 bv[LOADS], cv[LOADS];
+    const auto rows_left = [&](int c) {  // (of the chunk: its rows, and the first one)
+        const int first = (piece.hist ? (back ? c - nt : c) : back ? c : c - nh) * CHUNK;
+        const int64_t at = !back ? us.kv0 + first : us.q0 + (piece.hist ? us.L - 1 - first : (args.full ? us.L : 0) + first);
+        struct { int n; int64_t at; } r = {min(CHUNK, (piece.hist ? us.L : us.T) - first), at};
+        return r;
+    };
+    const bool down = back && piece.hist;
+    const auto fetch = [&](int c) {
+        const auto r = rows_left(c);
+        const int64_t first = (lowest(down, r.at) * heads + head) * D;
+        const char *b = (const char*)(bg + first), *x = (const char*)(cg + first);
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int row = tid / C16 + i * PART;
+            const unsigned at = bytes_of(down, row, pitch, tid % C16 * 16);
+            bv[i] = cv[i] = bf16x8{};
+            if (row < r.n) bv[i] = *(const bf16x8*)(b + at), cv[i] = *(const bf16x8*)(x + at);
+        }
+    };
+    fetch(piece.c0);
+    fill_powers<NT>(powers_s, args.log_decay + qh, 1, args.scale, tid);
+    const float *power = powers_s, *scaled = powers_s + POWERS;
+    Lane<D> at(tid, l16, quad, wave);
+    State<D> S;
+    S.zero();
+    for (int c = piece.c0; c < piece.c1; c++) {
+        const int n = rows_left(c).n;
+        at.forget(tid, l16, quad);
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            lds<bf16x8>(b_s + i * PART * (D * 2), at.stage) = bv[i];
+            lds<bf16x8>(c_s + i * PART * (D * 2), at.stage) = cv[i];
+        }
+        __syncthreads();
+        if (c + 1 < piece.c1) fetch(c + 1);
+        bf16x8 ct[2];
+#pragma unroll
+        for (int k = 0; k < 2; k++) ct[k] = read_tr<D>(c_s + 32 * k * (D * 2), at.tr);
+        if (piece.hist) S.keep(power[ZERO + n]);
+        S.add(b_s, ct, back ? scaled + ZERO + (piece.hist ? n : 1) : power + ZERO + n - 1, piece.hist ? 1 : 0, at, quad);
+        __syncthreads();
+    }
+    S.store((back ? args.states_back : args.states) + state_index(args, u, qh, piece.state) * D * D, wave, l16, quad);
+}
+
+// The states in front of the pieces from what each adds, in the order of the sweep: X <- l^n X + U, in place; the last is the caller's.  blockIdx.z: 1 backwards.
+constexpr int SCAN_THREADS = 256;
+template <int D>
+__global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const Args args, int first_job, const float* in_ahead, int transposed, float* out_ahead, const float* in_back,
+                                                            float* out_back) {
+    const bool back = (int)blockIdx.z + first_job == 1;
+    const int u = blockIdx.x / args.Hq, h = blockIdx.x % args.Hq, e = (blockIdx.y * SCAN_THREADS + threadIdx.x) * 4;
+    const User us = user_of(args, u);
+    const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK, seg = args.seg, rows = seg * CHUNK;
+    const int hs = (nh + seg - 1) / seg, ts = back ? (nt + seg - 1) / seg : 0, n = hs + ts;
+    const float g2 = fmaxf(fminf(args.log_decay[h], 0.f) * hta::LOG2E, MIN_LOG2), all = fast_exp2(g2 * (float)rows);
+    const float last = fast_exp2(g2 * (float)(us.L - (hs - 1) * rows));
+    const int64_t state = ((int64_t)u * args.Hq + h) * D * D;
+    const float* in = back ? in_back : in_ahead;
+    float* out = back ? out_back : out_ahead;
+    float* p = (back ? args.states_back : args.states) + state_index(args, u, h, 0) * D * D + e;
+    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+    if (in) {
+        if (!back && transposed)
+#pragma unroll
+            for (int v = 0; v < 4; v++) x[v] = in[state + ((e + v) % D) * D + (e + v) / D];
+        else x = *(const floatx4*)(in + state + e);
+    }
+    const bool adds = args.full || !back;  // (backwards through a history that does not ask nothing is added)
+    for (int s = 0; s < n; s += 4) {
+        floatx4 y[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) y[i] = s + i < n && (adds || s + i < ts) ? *(const floatx4*)(p + (int64_t)(s + i) * D * D) : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if (s + i >= n) break;
+            const float f = s + i < ts ? 1.f : s + i == n - 1 ? last : all;
+            *(floatx4*)(p + (int64_t)(s + i) * D * D) = x;
+            x = x * f + y[i];
+        }
+    }
+    *(floatx4*)(p + (int64_t)n * D * D) = x;
+    if (out) *(floatx4*)(out + state + e) = x;
+}
+
 // dk, dv = the sum of a group's shares, for the rows of the users
-constexpr int SUM_THREADS = 256, SUM_BLOCKS = 8;  // (per user)
+constexpr int SUM_THREADS = 256, SUM_BLOCKS = 16;  // (per user)
 __global__ __launch_bounds__(SUM_THREADS) void sum_kernel(const Args args, int d) {
     const User us = user_of(args, blockIdx.x);
-    const Pass& ps = args.pass[blockIdx.z];
+    const float* partial = blockIdx.z ? args.partial_k : args.partial_v;
+    __bf16* out = blockIdx.z ? args.dk : args.dv;
     const int64_t row = (int64_t)args.Hkv * d, slab = args.total_kv * row, first = us.kv0 * row, n = (int64_t)(us.L + us.T) * row;
-    for (int64_t e = ((int64_t)blockIdx.y * SUM_THREADS + threadIdx.x) * 8; e < n; e += (int64_t)SUM_BLOCKS * SUM_THREADS * 8) {
-        floatx4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-        for (int s = 0; s < args.spread; s++) {
-            lo += *(const floatx4*)(ps.partial + s * slab + first + e);
-            hi += *(const floatx4*)(ps.partial + s * slab + first + e + 4);
-        }
-        bf16x8 o;
+    for (int64_t e = ((int64_t)blockIdx.y * SUM_THREADS + threadIdx.x) * 4; e < n; e += (int64_t)SUM_BLOCKS * SUM_THREADS * 4) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < args.spread; s += 4) {
+            floatx4 y[4];
 #pragma unroll
-        for (int j = 0; j < 4; j++) o[j] = (__bf16)lo[j], o[4 + j] = (__bf16)hi[j];
-        *(bf16x8*)(ps.out + first + e) = o;
+            for (int i = 0; i < 4; i++) y[i] = s + i < args.spread ? __builtin_nontemporal_load((const floatx4*)(partial + (s + i) * slab + first + e)) : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 4; i++) x += y[i];
+        }
+        bf16x4 o;
+#pragma unroll
+        for (int j = 0; j < 4; j++) o[j] = (__bf16)x[j];
+        *(bf16x4*)(out + first + e) = o;
     }
 }
 
@@ -521,6 +819,9 @@ int check_sizes(int layer, int dtype, int32_t batch, int64_t total_q, int64_t to
     return MTFM_HTA_OK;
 }
 
+constexpr int MIN_SEG = 4;  // chunks of a piece at least
+constexpr int PER_CU(int d) { return d == 128 ? 2 : 4; }  // workgroups that a compute unit holds
+
 // heads of a group that a backward workgroup holds: what registers allow of the largest power of two that divides the group
 int heads_per_workgroup(int ratio, int d) {
     const int most = d == 128 ? 2 : 4;
@@ -530,42 +831,88 @@ int heads_per_workgroup(int ratio, int d) {
 }
 
 struct Plan {
-    int G, spread;
-    size_t partial;  // bytes of one slab set (dk or dv)
+    int G, spread;      // backwards: heads of a group to a workgroup, workgroups to a group
+    size_t partial;     // bytes of dk's (dv's) shares, 0 for none
+    int seg, n_hist, n_tgt;
+    size_t states;      // bytes of the pieces' states, one direction
 };
-Plan plan_backward(int64_t total_kv, int Hq, int Hkv, int d) {
-    Plan p;
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+Plan plan_of(bool backward, int batch, int64_t total_kv, int max_hist, int max_targets, int Hq, int Hkv, int d) {
+    Plan p = {};
     p.G = heads_per_workgroup(Hq / Hkv, d);
     p.spread = Hq / Hkv / p.G;
-    p.partial = p.spread > 1 ? align256((size_t)p.spread * total_kv * Hkv * d * sizeof(float)) : 0;
+    p.partial = backward && p.spread > 1 ? align256((size_t)p.spread * total_kv * Hkv * d * sizeof(float)) : 0;
+    // Pieces: where users' heads do not fill the chip, a user's history is cut until they do.
+    const int places = 256 * PER_CU(d);
+    const int64_t whole = (int64_t)batch * Hq;
+    const int chunks = ceil_div(max_hist, CHUNK);
+    const int64_t cuts = places / whole;
+    if (cuts >= 2 && chunks >= 2 * MIN_SEG) {
+        p.seg = ceil_div(chunks, cuts) < MIN_SEG ? MIN_SEG : ceil_div(chunks, cuts);
+        p.n_hist = ceil_div(chunks, p.seg), p.n_tgt = ceil_div(ceil_div(max_targets, CHUNK), p.seg);
+        p.states = align256((size_t)whole * (p.n_hist + p.n_tgt + 1) * d * d * sizeof(float));
+    }
     return p;
 }
 
-template <int D, int G, int CB, bool BACK>
-hipError_t launch_sweep_as(const Args& a, hipStream_t s) {
-    const int64_t members = (int64_t)(BACK ? a.spread : a.ratio) * a.n_pass, groups = (int64_t)a.batch * a.Hkv;
-    const int64_t grid = (groups + hta::N_XCD - 1) / hta::N_XCD * hta::N_XCD * members;
-    hipLaunchKernelGGL((sweep_kernel<D, G, CB, BACK>), dim3((unsigned)grid), dim3(D * 4 / CB), 0, s, a);
+int64_t grid_of(const Args& a, int members) {
+    const int64_t units = (int64_t)a.batch * a.Hkv * (a.seg ? a.n_hist + a.n_tgt : 1);
+    return (units + hta::N_XCD - 1) / hta::N_XCD * hta::N_XCD * members;
+}
+
+template <int D>
+hipError_t launch_sweep_d(const Args& a, hipStream_t s) {
+    hipLaunchKernelGGL((sweep_kernel<D>), dim3((unsigned)grid_of(a, a.ratio)), dim3(D * 4), 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_sweep(const Args& a, int d, hipStream_t s) {
+    return d == 32 ? launch_sweep_d<32>(a, s) : d == 64 ? launch_sweep_d<64>(a, s) : launch_sweep_d<128>(a, s);
+}
+
+// first_job, jobs: 0, 1 the sweep in the tokens' order; 1, 1 backwards; 0, 2 both
+template <int D>
+hipError_t launch_states_d(const Args& a, int first_job, int jobs, const float* in_ahead, float* out_ahead, const float* in_back, float* out_back, hipStream_t s) {
+    hipLaunchKernelGGL((states_kernel<D>), dim3((unsigned)grid_of(a, a.ratio), jobs), dim3(D * 4), 0, s, a, first_job);
+    hipLaunchKernelGGL((scan_kernel<D>), dim3(a.batch * a.Hq, D * D / (SCAN_THREADS * 4), jobs), dim3(SCAN_THREADS), 0, s, a, first_job, in_ahead, a.transposed,
+                       out_ahead, in_back, out_back);
+    return hipGetLastError();
+}
+hipError_t launch_states(const Args& a, int d, int first_job, int jobs, const float* in_ahead, float* out_ahead, const float* in_back, float* out_back, hipStream_t s) {
+    const auto launch = d == 32 ? launch_states_d<32> : d == 64 ? launch_states_d<64> : launch_states_d<128>;
+    hta::timing_begin(MTFM_HLA_KERNEL_STATES, s);
+    const hipError_t e = launch(a, first_job, jobs, in_ahead, out_ahead, in_back, out_back, s);
+    hta::timing_end(MTFM_HLA_KERNEL_STATES, s);
+    return e;
+}
+
+// Lets a kernel use its dynamic LDS; asked for once per kernel, not a stream operation (a graph that is being captured does not see it).
+template <auto Kernel>
+hipError_t allow_lds(int bytes) {
+    static hipError_t state = hipFuncSetAttribute((const void*)Kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return state;
+}
+template <int D, int G>
+hipError_t launch_back_as(const Args& a, hipStream_t s) {
+    constexpr int lds = back_lds<D, G>();
+    if (hipError_t e = allow_lds<back_kernel<D, G>>(lds); e != hipSuccess) return e;
+    hipLaunchKernelGGL((back_kernel<D, G>), dim3((unsigned)grid_of(a, a.spread)), dim3(D * 4), lds, s, a);
     return hipGetLastError();
 }
 template <int D>
-hipError_t launch_sweep_d(const Args& a, bool back, int G, hipStream_t s) {
-    if (!back) return launch_sweep_as<D, 1, 1, false>(a, s);
-    if (G == 1) return launch_sweep_as<D, 1, 1, true>(a, s);
-    if (G == 2) return launch_sweep_as<D, 2, 1, true>(a, s);
-    if constexpr (D < 128) return launch_sweep_as<D, 4, 1, true>(a, s);
-    return hipErrorInvalidValue;
+hipError_t launch_back_d(const Args& a, int G, hipStream_t s) {
+    return G == 1 ? launch_back_as<D, 1>(a, s) : G == 2 ? launch_back_as<D, 2>(a, s) : launch_back_as<D, 4>(a, s);
 }
-hipError_t launch_sweep(const Args& a, int d, bool back, int G, hipStream_t s) {
-    return d == 32 ? launch_sweep_d<32>(a, back, G, s) : d == 64 ? launch_sweep_d<64>(a, back, G, s) : launch_sweep_d<128>(a, back, G, s);
+hipError_t launch_back(const Args& a, int d, int G, hipStream_t s) {
+    return d == 32 ? launch_back_d<32>(a, G, s) : d == 64 ? launch_back_d<64>(a, G, s) : launch_back_d<128>(a, G, s);
 }
 
 Args args_of(const float* log_decay, const int32_t* q_offsets, const int32_t* kv_offsets, const int32_t* hist_len, const int32_t* n_targets, int32_t batch,
-             int64_t total_q, int64_t total_kv, int32_t Hq, int32_t Hkv, float scale, int layer) {
+             int64_t total_q, int64_t total_kv, int32_t max_hist, int32_t max_targets, int32_t Hq, int32_t Hkv, float scale, int layer) {
     Args a = {};
     a.log_decay = log_decay, a.q_off = q_offsets, a.kv_off = kv_offsets, a.hist_len = hist_len, a.n_targets = n_targets;
-    a.total_q = total_q, a.total_kv = total_kv, a.batch = batch, a.Hq = Hq, a.Hkv = Hkv, a.ratio = Hq / Hkv, a.n_pass = 1, a.spread = 1;
-    a.full = layer == MTFM_HTA_LAYER_FULL, a.scale = scale;
+    a.total_q = total_q, a.total_kv = total_kv, a.batch = batch, a.Hq = Hq, a.Hkv = Hkv, a.ratio = Hq / Hkv, a.spread = 1;
+    a.full = layer == MTFM_HTA_LAYER_FULL, a.max_hist = max_hist, a.max_targets = max_targets, a.scale = scale;
     return a;
 }
 
@@ -611,8 +958,9 @@ extern "C" {
 size_t mtfm_hla_workspace_bytes(int layer, int dtype, int is_bwd, int32_t batch, int64_t total_q, int64_t total_kv, int32_t max_hist, int32_t max_targets,
                                 int32_t Hq, int32_t Hkv, int32_t head_dim) {
     if (hla::check_sizes(layer, dtype, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, head_dim) != MTFM_HTA_OK) return (size_t)-1;
-    if (!is_bwd || batch == 0) return 0;
-    return 2 * hla::plan_backward(total_kv, Hq, Hkv, head_dim).partial;
+    if (batch == 0) return 0;
+    const hla::Plan plan = hla::plan_of(is_bwd, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
+    return 2 * plan.partial + (is_bwd ? 2 : 1) * plan.states;
 }
 
 int mtfm_hla_fwd(const void* q, const void* k, const void* v, const float* log_decay, const float* state, void* out, float* final_state,
@@ -622,12 +970,19 @@ int mtfm_hla_fwd(const void* q, const void* k, const void* v, const float* log_d
     if (int rc = hla::check_sizes(layer, dtype, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, head_dim)) return rc;
     if (batch == 0) return MTFM_HTA_OK;
     if (int rc = hla::check_arrays({q, out}, {k, v}, {state, final_state}, log_decay, {q_offsets, kv_offsets, hist_len, n_targets}, total_q, total_kv, scale)) return rc;
-    hla::Args a = hla::args_of(log_decay, q_offsets, kv_offsets, hist_len, n_targets, batch, total_q, total_kv, Hq, Hkv, scale, layer);
-    a.pass[0] = {(const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (__bf16*)out, nullptr, state, final_state, 0};
+    const hla::Plan plan = hla::plan_of(false, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
+    if (int rc = hla::check_workspace(plan.states, workspace, workspace_bytes)) return rc;
+    hla::Args a = hla::args_of(log_decay, q_offsets, kv_offsets, hist_len, n_targets, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, scale, layer);
+    a.seg = plan.seg, a.n_hist = plan.n_hist, a.n_tgt = plan.n_tgt, a.states = (float*)workspace;
+    a.a = (const __bf16*)q, a.b = (const __bf16*)k, a.c = (const __bf16*)v, a.out = (__bf16*)out, a.state_in = state, a.state_out = final_state;
     hipStream_t s = (hipStream_t)stream;
-    hta::timing_begin(MTFM_HLA_KERNEL_FWD, s);
-    const hipError_t e = hla::launch_sweep(a, head_dim, false, 1, s);
-    hta::timing_end(MTFM_HLA_KERNEL_FWD, s);
+    hipError_t e = hipSuccess;
+    if (plan.seg) e = hla::launch_states(a, head_dim, 0, 1, state, final_state, nullptr, nullptr, s);
+    if (e == hipSuccess && (total_q > 0 || !plan.seg)) {
+        hta::timing_begin(MTFM_HLA_KERNEL_FWD, s);
+        e = hla::launch_sweep(a, head_dim, s);
+        hta::timing_end(MTFM_HLA_KERNEL_FWD, s);
+    }
     if (e != hipSuccess) return hta::report_error(MTFM_HTA_ERR_LAUNCH, "linear attention forward launch: %s", hipGetErrorString(e));
     return MTFM_HTA_OK;
 }
@@ -641,23 +996,25 @@ int mtfm_hla_bwd(const void* dout, const void* q, const void* k, const void* v, 
     if (int rc = hla::check_arrays({dout, q, dq}, {k, v, dk, dv}, {state, dfinal_state, dstate}, log_decay, {q_offsets, kv_offsets, hist_len, n_targets}, total_q,
                                    total_kv, scale))
         return rc;
-    const hla::Plan plan = hla::plan_backward(total_kv, Hq, Hkv, head_dim);
-    if (int rc = hla::check_workspace(2 * plan.partial, workspace, workspace_bytes)) return rc;
-    hla::Args a = hla::args_of(log_decay, q_offsets, kv_offsets, hist_len, n_targets, batch, total_q, total_kv, Hq, Hkv, scale, layer);
+    const hla::Plan plan = hla::plan_of(true, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
+    if (int rc = hla::check_workspace(2 * plan.partial + 2 * plan.states, workspace, workspace_bytes)) return rc;
+    hla::Args a = hla::args_of(log_decay, q_offsets, kv_offsets, hist_len, n_targets, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, scale, layer);
     hipStream_t s = (hipStream_t)stream;
     const auto Q = (const __bf16*)q, K = (const __bf16*)k, V = (const __bf16*)v, dO = (const __bf16*)dout;
     hipError_t e = hipSuccess;
+    a.q = Q, a.k = K, a.v = V, a.dout = dO, a.dk = (__bf16*)dk, a.dv = (__bf16*)dv, a.b = V, a.c = K, a.transposed = 1;
+    a.seg = plan.seg, a.n_hist = plan.n_hist, a.n_tgt = plan.n_tgt;
+    a.states = (float*)((char*)workspace + 2 * plan.partial), a.states_back = a.states + plan.states / sizeof(float);
+    if (plan.seg) e = hla::launch_states(a, head_dim, total_q > 0 ? 0 : 1, total_q > 0 ? 2 : 1, state, nullptr, dfinal_state, dstate, s);
     hta::timing_begin(MTFM_HLA_KERNEL_BWD, s);
-    if (total_q > 0) {
-        a.pass[0] = {dO, V, K, (__bf16*)dq, nullptr, state, nullptr, 1};
-        e = hla::launch_sweep(a, head_dim, false, 1, s);
+    if (e == hipSuccess && total_q > 0) {
+        a.a = dO, a.out = (__bf16*)dq, a.state_in = state;
+        e = hla::launch_sweep(a, head_dim, s);
     }
     if (e == hipSuccess) {
-        float* partial = plan.spread > 1 ? (float*)workspace : nullptr;
-        a.pass[0] = {K, Q, dO, (__bf16*)dv, partial, dfinal_state, dstate, 0};
-        a.pass[1] = {V, dO, Q, (__bf16*)dk, partial ? partial + plan.partial / sizeof(float) : nullptr, dfinal_state, nullptr, 1};
-        a.n_pass = 2, a.spread = plan.spread;
-        e = hla::launch_sweep(a, head_dim, true, plan.G, s);
+        a.state_in = dfinal_state, a.state_out = dstate, a.spread = plan.spread;
+        if (plan.spread > 1) a.partial_k = (float*)workspace, a.partial_v = a.partial_k + plan.partial / sizeof(float);
+        e = hla::launch_back(a, head_dim, plan.G, s);
     }
     hta::timing_end(MTFM_HLA_KERNEL_BWD, s);
     if (e == hipSuccess && plan.spread > 1 && total_kv > 0) {
