@@ -25,7 +25,7 @@ using hta::bf16x8;
 using hta::fast_exp2;
 using hta::floatx4;
 
-constexpr int CHUNK = 64;
+constexpr int MOST_ROWS = 64;  // of a chunk
 constexpr float MIN_LOG2 = -1e4f;  // of a decay: 2^-10000 is 0, and 0 times it is not NaN
 
 // A sweep in the tokens' order: the forward pass, or dq
@@ -46,17 +46,18 @@ struct Args {
     __bf16 *dk, *dv;
     float *partial_k, *partial_v;  // where a group's heads are spread over workgroups: [spread][total_kv][Hkv][d] each; null otherwise
     int32_t spread;
-    // long histories in pieces (seg > 0): `seg` chunks of one kind to a workgroup, at most n_hist pieces of a history and n_tgt of a user's candidates.  The
+    // long histories in pieces (seg > 0): `seg` rows of one kind to a workgroup, at most n_hist pieces of a history and n_tgt of a user's candidates.  The
     // states in front of the pieces lie in [batch][Hq][n_hist + n_tgt + 1][d][d], in the order of the sweep (backwards the candidates' come first), and the one
     // behind them all.
     int32_t seg, n_hist, n_tgt;
     float *states, *states_back;
+    const int32_t* order;  // users by decreasing work; null: as they come
 };
 
-// What of a user a workgroup has: chunks [c0, c1) of the sweep, and the index of the state in front of them (-1, without pieces: what the caller gave)
+// What of a user a workgroup has: rows [h0, h1) of the history in the sweep's order, candidates [t0, t1), and the index of the state in front of them (-1, without
+// pieces: what the caller gave)
 struct Piece {
-    int c0, c1, state;
-    bool hist;
+    int h0, h1, t0, t1, state;
 };
 __device__ inline int64_t state_index(const Args& g, int u, int h, int i) { return ((int64_t)u * g.Hq + h) * (g.n_hist + g.n_tgt + 1) + i; }
 // Which user, key/value head, piece and member (query head, or set of them) a workgroup has: those that share rows are neighbours on one XCD, and pieces go around
@@ -69,21 +70,15 @@ __device__ inline bool place_of(const Args& g, int members, Place& w) {
     const int64_t unit = (int64_t)(slot / members) * hta::N_XCD + xcd;
     if (unit >= (int64_t)g.batch * g.Hkv * pieces) return false;
     const int group = (int)(unit / pieces);
-    w.u = group / g.Hkv, w.kvh = group % g.Hkv, w.member = slot % members, w.piece = (int)(unit % pieces);
+    w.u = g.order ? g.order[group / g.Hkv] : group / g.Hkv, w.kvh = group % g.Hkv, w.member = slot % members, w.piece = (int)(unit % pieces);
     return true;
 }
-__device__ inline Piece piece_of(const Args& g, int id, int nh, int nt, bool back) {
-    Piece p;
-    if (g.seg == 0) {
-        p.c0 = 0, p.c1 = nh + nt, p.state = -1, p.hist = true;
-        return p;
-    }
-    p.hist = id < g.n_hist;
-    const int n = p.hist ? nh : nt, first = (p.hist ? id : id - g.n_hist) * g.seg, ahead = p.hist == back ? (back ? nt : nh) : 0;
-    p.c0 = ahead + min(first, n), p.c1 = ahead + min(first + g.seg, n);
-    if (back) p.state = p.hist ? (nt + g.seg - 1) / g.seg + id : id - g.n_hist;
-    else p.state = p.hist ? id : (nh + g.seg - 1) / g.seg;
-    return p;
+__device__ inline Piece piece_of(const Args& g, int id, int L, int T, bool back) {
+    if (g.seg == 0) return {0, L, 0, T, -1};
+    const int hs = (L + g.seg - 1) / g.seg, ts = (T + g.seg - 1) / g.seg;
+    if (id < g.n_hist) return {min(id * g.seg, L), min((id + 1) * g.seg, L), 0, 0, back ? ts + id : id};
+    id -= g.n_hist;
+    return {0, 0, min(id * g.seg, T), min((id + 1) * g.seg, T), back ? id : hs};
 }
 
 // Tiles in LDS lie in rows of D elements without padding; the 16-byte word w of row r is at position w ^ place<D>(r).  A 16-byte read is served in groups of
@@ -155,7 +150,7 @@ __device__ inline bf16x8 read_tr(char* tile, unsigned at) {
     return hta::lds_read_tr_pair((const __bf16*)(tile + at), (const __bf16*)(tile + (at ^ 32) + 4 * D * 2));
 }
 
-constexpr int ZERO = CHUNK, POWERS = 2 * CHUNK + 4;  // powers of a decay: entry ZERO + m holds l^m, m = -64 .. 64, 0 for m < 0
+constexpr int ZERO = MOST_ROWS, POWERS = 2 * MOST_ROWS + 4;  // powers of a decay: entry ZERO + m holds l^m, m = -64 .. 64, 0 for m < 0
 // the tables of `heads` heads from h on, [plain | times scale] each
 template <int NT>
 __device__ inline void fill_powers(float* table, const float* log_decay, int heads, float scale, int tid) {
@@ -168,8 +163,8 @@ __device__ inline void fill_powers(float* table, const float* log_decay, int hea
 }
 
 // One tile of P^T = B A^T with the decays, rows i = 16 it .. of A (queries), rows j = 16 jt .. of B, to P[i][j]
-template <int D>
-__device__ inline void score_tile(char* a, char* b, char* p_tile, const float* scaled, const Lane<D>& at, const Lane<CHUNK>& at_p, int it, int jt, int l16, int quad) {
+template <int D, int C>
+__device__ inline void score_tile(char* a, char* b, char* p_tile, const float* scaled, const Lane<D>& at, const Lane<C>& at_p, int it, int jt, int l16, int quad) {
     floatx4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < D / 32; k++)
@@ -187,38 +182,42 @@ __device__ inline void score_tile(char* a, char* b, char* p_tile, const float* s
     }
     // word 2 jt + quad / 2 of row i, its half quad % 2: from word quad
     const unsigned to = (at_p.row ^ ((quad ^ (quad >> 1)) * 16) ^ (32 * jt)) + (quad & 1) * 8;
-    lds<bf16x4>(p_tile + it * (16 * CHUNK * 2), to) = p;
+    lds<bf16x4>(p_tile + it * (16 * C * 2), to) = p;
 }
 __device__ inline int tile_row(int t) { return t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0; }  // of the ten tiles on and below the diagonal
 
-// C^T P^T for rows 16 it .. of a chunk: what its own rows add.  `odd`: an infinity or a NaN in c reaches all rows as 0 times itself, the last ones in any case
-// (so they come first); then it is done row by row.
-template <int D, int IT>
-__device__ inline floatx4 within_chunk(const bf16x8 (&ct)[2], char* p_tile, char* c_tile, const Lane<CHUNK>& at_p, int block, bool& odd, int l16, int quad) {
-    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+// C^T P^T: what a chunk's own rows add, rows 16 it .. to x[it].  An infinity or a NaN in c would reach the rows in front of it as 0 times itself; it reaches the
+// last rows in any case, and where those are not finite all of it is done again, row by row.
+template <int D, int C>
+__device__ inline void within_chunk(floatx4 (&x)[C / 16], const bf16x8 (&ct)[C / 32], char* p_tile, char* c_tile, const Lane<C>& at_p, int block, int l16, int quad) {
+    constexpr int IT = C / 16;
 #pragma unroll
-    for (int k = 0; k <= IT / 2; k++) x = mfma16(ct[k], lds<bf16x8>(p_tile + IT * (16 * CHUNK * 2), at_p.row ^ (64 * k)), x);
-    if (IT == 3) {
-        const float zero = fmaf(x[0], 0.f, x[1] * 0.f) + fmaf(x[2], 0.f, x[3] * 0.f);
-        odd = __ballot(zero != zero) != 0;
+    for (int it = 0; it < IT; it++) {
+        x[it] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k <= it / 2; k++) x[it] = mfma16(ct[k], lds<bf16x8>(p_tile + it * (16 * C * 2), at_p.row ^ (64 * k)), x[it]);
     }
-    if (odd) {
-        const int i = 16 * IT + l16;
-        x = floatx4{0.f, 0.f, 0.f, 0.f};
-        for (int j = 0; j < 16 * IT + 16; j++) {
-            const float p = (float)lds<__bf16>(p_tile, i * (CHUNK * 2) + (((j / 8) ^ place<CHUNK>(i)) * 16) + (j & 7) * 2);
+    const float zero = fmaf(x[IT - 1][0], 0.f, x[IT - 1][1] * 0.f) + fmaf(x[IT - 1][2], 0.f, x[IT - 1][3] * 0.f);
+    if (__ballot(zero != zero) != 0) {
+#pragma unroll
+        for (int it = 0; it < IT; it++) x[it] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < C; j++) {
             const bf16x4 c = lds<bf16x4>(c_tile, j * (D * 2) + (((2 * block + (quad >> 1)) ^ place<D>(j)) * 16) + (quad & 1) * 8);
 #pragma unroll
-            for (int v = 0; v < 4; v++) x[v] += j <= i ? p * (float)c[v] : 0.f;
+            for (int it = 0; it < IT; it++) {
+                const int i = 16 * it + l16;
+                const float p = (float)lds<__bf16>(p_tile, i * (C * 2) + (((j / 8) ^ place<C>(i)) * 16) + (j & 7) * 2);
+#pragma unroll
+                for (int v = 0; v < 4; v++) x[it][v] += j <= i ? p * (float)c[v] : 0.f;
+            }
         }
     }
-    return x;
 }
 
-// candidates: <a_i, b_i> scale to dots[i], NT / 64 lanes to a row
-template <int D, int NT>
+// candidates: <a_i, b_i> scale to dots[i], NT / C lanes to a row
+template <int D, int C, int NT>
 __device__ inline void own_dots(char* a, char* b, float* dots, float scale, int tid) {
-    constexpr int LANES = NT / CHUNK, WORDS = D / 8 / LANES;
+    constexpr int LANES = NT / C, WORDS = D / 8 / LANES;
     const int row = tid / LANES, part = tid % LANES;
     float dot = 0.f;
 #pragma unroll
@@ -274,11 +273,13 @@ struct State {
 #pragma unroll
             for (int v = 0; v < 4; v++) s[k][v] = (__bf16)t[2 * k][v], s[k][4 + v] = (__bf16)t[2 * k + 1][v];
     }
-    // += B^T (w c): w c goes in as two bf16 values, so that float32 keeps 16 bits of it.  w[-j]: the weight of row j (rows that are not there are zero,
-    // and so are the weights behind the table's end); step 0: the same for all.
-    __device__ void add(char* b_tile, const bf16x8 (&ct)[2], const float* w, int step, const Lane<D>& at, int quad) {
+    // += B^T (w c): w c goes in as two bf16 values, 16 bits of it, or as three, all of float32's, where the state itself is what the caller gets (`whole`).
+    // w[-j]: the weight of row j (rows that are not there are zero, and so are the weights behind the table's end); step 0: the same for all.
+    template <int KT, typename Step>
+    __device__ void add(char* b_tile, const bf16x8 (&ct)[KT], const float* w, Step, const Lane<D>& at, int quad, bool whole) {
+        constexpr int step = Step::value;
 #pragma unroll
-        for (int k = 0; k < 2; k++) {
+        for (int k = 0; k < KT; k++) {
             const float* p = w - step * (32 * k + 8 * quad);
             float x[8];
 #pragma unroll
@@ -291,14 +292,29 @@ struct State {
                 t[i] = mfma16(bt, hi, t[i]);
                 t[i] = mfma16(bt, lo, t[i]);
             }
+            if (!whole) continue;
+            bf16x8 rest;
+#pragma unroll
+            for (int e = 0; e < 8; e++) rest[e] = (__bf16)(x[e] - (float)hi[e] - (float)lo[e]);
+#pragma unroll
+            for (int i = 0; i < TILES; i++)
+                t[i] = mfma16(read_tr<D>(b_tile + 32 * k * (D * 2) + 8 * (i % 2), at.trp ^ (64 * (i / 2))), rest, t[i]);
         }
     }
 };
 
-// A chunk's rows in memory: a uniform address, that of the lowest of 64 rows (backwards through a history row 63, which need not be there), and a lane's
+// A chunk's rows in memory: a uniform address, that of the lowest of C rows (backwards through a history row C - 1, which need not be there), and a lane's
 // bytes from there
-__device__ inline int64_t lowest(bool down, int64_t first) { return down ? first - (CHUNK - 1) : first; }
-__device__ inline unsigned bytes_of(bool down, int r, unsigned pitch, int byte) { return __umul24(down ? CHUNK - 1 - r : r, pitch) + byte; }
+template <int C>
+__device__ inline int64_t lowest(bool down, int64_t first) { return down ? first - (C - 1) : first; }
+template <int C>
+__device__ inline unsigned bytes_of(bool down, int r, unsigned pitch, int byte) { return __umul24(down ? C - 1 - r : r, pitch) + byte; }
+
+// What a chunk's rows are: a history's that ask, a history's that do not (a target-only layer), candidates.  The loops have a body for each: branches inside a
+// body leave accumulators to be moved about.
+enum Kind { ASKING, SILENT, CANDIDATES };
+template <Kind K>
+using KindOf = std::integral_constant<Kind, K>;
 
 struct Rows {  // of a chunk: n rows, row r is first + r (backwards through a history: first - r)
     int64_t q, kv;
@@ -308,11 +324,11 @@ struct Rows {  // of a chunk: n rows, row r is first + r (backwards through a hi
 
 // One sweep over a user's head in the tokens' order by a workgroup of D / 16 waves, each with 16 of the state's columns.  D[m][n] += A[m][k] B[k][n] of
 // 16x16x32: a lane holds row (column) lane % 16 and k = 8 (lane / 16) .. + 7 of either operand, and column lane % 16, rows 4 (lane / 16) .. + 3 of the result.
-template <int D>
-__global__ __launch_bounds__(D * 4, D == 128 ? 2 : 4) void sweep_kernel(const Args args) {
-    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = CHUNK / PART, TILE = CHUNK * D * 2;
-    __shared__ __attribute__((aligned(16))) char a_s[TILE], b_s[TILE], c_s[TILE], p_s[CHUNK * CHUNK * 2];
-    __shared__ float dots_s[CHUNK], powers_s[2 * POWERS];
+template <int D, int C, bool FULL>
+__global__ __launch_bounds__(D * 4, 4) void sweep_kernel(const Args args) {
+    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = C / PART, TILE = C * D * 2, IT = C / 16, KT = C / 32, TILES = IT * (IT + 1) / 2;
+    __shared__ __attribute__((aligned(16))) char a_s[TILE], b_s[TILE], c_s[TILE], p_s[C * C * 2];
+    __shared__ float dots_s[C], powers_s[2 * POWERS];
     int tid = threadIdx.x, l16 = tid & 15, quad = (tid >> 4) & 3;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -320,10 +336,9 @@ __global__ __launch_bounds__(D * 4, D == 128 ? 2 : 4) void sweep_kernel(const Ar
     if (!place_of(args, args.ratio, place)) return;
     const int u = place.u, kvh = place.kvh, qh = kvh * args.ratio + place.member;
     const User us = user_of(args, u);
-    const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK;
-    const bool full = args.full;
-    const Piece piece = piece_of(args, place.piece, nh, nt, false);
-    if (args.seg && (piece.c0 >= piece.c1 || (piece.hist && !full))) return;
+    const Piece piece = piece_of(args, place.piece, us.L, us.T, false);
+    const int nh = (piece.h1 - piece.h0 + C - 1) / C, chunks = nh + (piece.t1 - piece.t0 + C - 1) / C;
+    if (args.seg && (chunks == 0 || (nh > 0 && !FULL))) return;
 
     State<D> S;
     if (piece.state >= 0) S.load(args.states + state_index(args, u, qh, piece.state) * D * D, false, wave, l16, quad);
@@ -333,9 +348,9 @@ __global__ __launch_bounds__(D * 4, D == 128 ? 2 : 4) void sweep_kernel(const Ar
     const auto rows_of = [&](int c) {
         Rows r;
         r.hist = c < nh;
-        const int first = (r.hist ? c : c - nh) * CHUNK;
-        r.n = min(CHUNK, (r.hist ? us.L : us.T) - first);
-        r.kv = us.kv0 + (r.hist ? 0 : us.L) + first, r.q = us.q0 + (!r.hist && full ? us.L : 0) + first;
+        const int first = r.hist ? piece.h0 + c * C : piece.t0 + (c - nh) * C;
+        r.n = min(C, (r.hist ? piece.h1 : piece.t1) - first);
+        r.kv = us.kv0 + (r.hist ? 0 : us.L) + first, r.q = us.q0 + (!r.hist && FULL ? us.L : 0) + first;
         return r;
     };
     // 16-byte words of the three tiles on their way: word tid % C16 of rows tid / C16 + i PART.  Rows that are not there are zero.
@@ -343,13 +358,13 @@ __global__ __launch_bounds__(D * 4, D == 128 ? 2 : 4) void sweep_kernel(const Ar
     bf16x8 av[LOADS], bv[LOADS], cv[LOADS];
     const auto fetch = [&](int chunk) {
         const Rows r = rows_of(chunk);
-        const bool asks = full || !r.hist;
+        const bool asks = FULL || !r.hist;
         const char* a = (const char*)(args.a + (r.q * args.Hq + qh) * D);
         const char *b = (const char*)(args.b + (r.kv * args.Hkv + kvh) * D), *c = (const char*)(args.c + (r.kv * args.Hkv + kvh) * D);
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
             const int row = tid / C16 + i * PART;
-            const unsigned at_a = bytes_of(false, row, pitch_q, tid % C16 * 16), at_b = bytes_of(false, row, pitch_kv, tid % C16 * 16);
+            const unsigned at_a = bytes_of<C>(false, row, pitch_q, tid % C16 * 16), at_b = bytes_of<C>(false, row, pitch_kv, tid % C16 * 16);
             av[i] = bv[i] = cv[i] = bf16x8{};
             if (row < r.n) {
                 if (asks) av[i] = *(const bf16x8*)(a + at_a);
@@ -358,74 +373,76 @@ __global__ __launch_bounds__(D * 4, D == 128 ? 2 : 4) void sweep_kernel(const Ar
         }
     };
 
-    if (piece.c0 < piece.c1) fetch(piece.c0);
+    if (chunks > 0) fetch(0);
     fill_powers<NT>(powers_s, args.log_decay + qh, 1, args.scale, tid);
     const float *power = powers_s, *scaled = powers_s + POWERS;
     // (entries of P that a product reads and no chunk writes)
-    for (int i = tid; i < CHUNK * CHUNK / 8; i += NT) ((bf16x8*)p_s)[i] = bf16x8{};
+    for (int i = tid; i < C * C / 8; i += NT) ((bf16x8*)p_s)[i] = bf16x8{};
     Lane<D> at(tid, l16, quad, wave);
-    Lane<CHUNK> at_p(0, l16, quad, 0);
+    Lane<C> at_p(0, l16, quad, 0);
 
-    for (int c = piece.c0; c < piece.c1; c++) {
+    const auto turn = [&](auto K, int c) {
+        constexpr Kind kind = decltype(K)::value;
         const Rows r = rows_of(c);
-        const bool asks = full || !r.hist;
         at.forget(tid, l16, quad);
         at_p.forget(tid, l16, quad);
         // (the last readers of the tiles are behind the barrier at the end of the turn)
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
-            lds<bf16x8>(a_s + i * PART * (D * 2), at.stage) = av[i];
+            if (kind != SILENT) lds<bf16x8>(a_s + i * PART * (D * 2), at.stage) = av[i];
             lds<bf16x8>(b_s + i * PART * (D * 2), at.stage) = bv[i];
             lds<bf16x8>(c_s + i * PART * (D * 2), at.stage) = cv[i];
         }
         __syncthreads();
-        if (c + 1 < piece.c1) fetch(c + 1);
-        if (r.hist && asks) {
+        if (c + 1 < chunks) fetch(c + 1);
+        if (kind == ASKING) {
 #pragma unroll
-            for (int t0 = 0; t0 < 10; t0 += NW) {
+            for (int t0 = 0; t0 < TILES; t0 += NW) {
                 const int t = t0 + wave, it = tile_row(t), jt = t - it * (it + 1) / 2;
-                if (t < 10) score_tile<D>(a_s, b_s, p_s, scaled, at, at_p, it, jt, l16, quad);
+                if (t0 + NW <= TILES || t < TILES) score_tile<D, C>(a_s, b_s, p_s, scaled, at, at_p, it, jt, l16, quad);
             }
-        } else if (!r.hist) {
-            own_dots<D, NT>(a_s, b_s, dots_s, args.scale, tid);
+        } else if (kind == CANDIDATES) {
+            own_dots<D, C, NT>(a_s, b_s, dots_s, args.scale, tid);
         }
         // o^T = S^T A^T, row i of it times l^(i+1) scale (candidates: l scale)
-        floatx4 o[4];
-        if (asks) {
+        floatx4 o[IT];
+        if (kind != SILENT) {
             bf16x8 s[KS];
             S.rounded(s);
 #pragma unroll
-            for (int it = 0; it < 4; it++)
+            for (int it = 0; it < IT; it++)
 #pragma unroll
                 for (int k = 0; k < KS; k++)
                     o[it] = mfma16(s[k], lds<bf16x8>(a_s + it * (16 * D * 2), at.row ^ (64 * k)), k == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : o[it]);
+            __syncthreads();
         }
-        __syncthreads();
-        bf16x8 ct[2];  // C^T: this wave's columns of c, rows 32 k + 8 quad .. + 7
+        bf16x8 ct[KT];  // C^T: this wave's columns of c, rows 32 k + 8 quad .. + 7
+        if (kind != CANDIDATES)
 #pragma unroll
-        for (int k = 0; k < 2; k++) ct[k] = read_tr<D>(c_s + 32 * k * (D * 2), at.tr);
-        if (asks) {
+            for (int k = 0; k < KT; k++) ct[k] = read_tr<D>(c_s + 32 * k * (D * 2), at.tr);
+        if (kind != SILENT) {
             char* out = (char*)(args.out + (r.q * args.Hq + qh) * D);
-            const float* f = scaled + ZERO + 1 + (r.hist ? l16 : 0);
-            const int step = r.hist ? 16 : 0;
-            bool odd = false;
-            hta::static_for<0, 4>([&](auto I) {
-                constexpr int it = 3 - decltype(I)::value;
-                const int i = 16 * it + l16;
-                const floatx4 x = r.hist ? within_chunk<D, it>(ct, p_s, c_s, at_p, wave, odd, l16, quad) : own_term<D>(dots_s, c_s, wave, i, quad);
-                const float w = f[it * step];
+            floatx4 x[IT];
+            if (kind == ASKING) within_chunk<D, C>(x, ct, p_s, c_s, at_p, wave, l16, quad);
+#pragma unroll
+            for (int it = 0; it < IT; it++) {
+                if (kind == CANDIDATES) x[it] = own_term<D>(dots_s, c_s, wave, 16 * it + l16, quad);
+                const float w = scaled[ZERO + 1 + (kind == ASKING ? 16 * it + l16 : 0)];
                 bf16x4 y;
 #pragma unroll
-                for (int v = 0; v < 4; v++) y[v] = (__bf16)fmaf(o[it][v], w, x[v]);
-                if (i < r.n) *(bf16x4*)(out + bytes_of(false, i, pitch_q, 32 * wave + 8 * quad)) = y;
-            });
+                for (int v = 0; v < 4; v++) y[v] = (__bf16)fmaf(o[it][v], w, x[it][v]);
+                if (16 * it + l16 < r.n) *(bf16x4*)(out + bytes_of<C>(false, 16 * it + l16, pitch_q, 32 * wave + 8 * quad)) = y;
+            }
         }
-        if (r.hist) {  // the state behind the chunk: l^n S + B^T (w c), w_j = l^(n-1-j)
+        if (kind != CANDIDATES) {  // the state behind the chunk: l^n S + B^T (w c), w_j = l^(n-1-j)
             S.keep(power[ZERO + r.n]);
-            S.add(b_s, ct, power + ZERO + r.n - 1, 1, at, quad);
+            S.add(b_s, ct, power + ZERO + r.n - 1, std::integral_constant<int, 1>{}, at, quad, args.state_out != nullptr);
         }
         __syncthreads();
-    }
+    };
+    int c = 0;
+    for (; c < nh; c++) turn(KindOf<FULL ? ASKING : SILENT>{}, c);
+    for (; c < chunks; c++) turn(KindOf<CANDIDATES>{}, c);
     if (args.state_out && !args.seg) S.store(args.state_out + ((int64_t)u * args.Hq + qh) * D * D, wave, l16, quad);
 }
 
@@ -434,12 +451,12 @@ __global__ __launch_bounds__(D * 4, D == 128 ? 2 : 4) void sweep_kernel(const Ar
 //   dv_i = l^i k_i R + scale sum_(j<=i) l^(i-j) <k_i, q_j> dout_j,     dk_i = l^i v_i R^T + scale sum_(j<=i) l^(i-j) <v_i, dout_j> q_j,
 //   R <- l^n R + scale sum_j l^(n-j) q_j dout_j^T.
 // A wave owns 16 columns of R, and the same columns of dv and of dk; R^T, which the latter needs, is R rounded in LDS, read transposed.
-template <int D, int G>
+template <int D, int G, int C, bool FULL>
 __global__ __launch_bounds__(D * 4, 2) void back_kernel(const Args args) {
-    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = CHUNK / PART, TILE = CHUNK * D * 2;
+    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = C / PART, TILE = C * D * 2, IT = C / 16, KT = C / 32, TILES = IT * (IT + 1) / 2;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    char *k_s = smem, *v_s = k_s + TILE, *q_s = v_s + TILE, *g_s = q_s + TILE, *pq_s = g_s + TILE, *pg_s = pq_s + CHUNK * CHUNK * 2, *r_s = pg_s + CHUNK * CHUNK * 2;
-    float *dots_q = (float*)(r_s + D * D * 2), *dots_g = dots_q + CHUNK, *powers_s = dots_g + CHUNK;
+    char *k_s = smem, *v_s = k_s + TILE, *q_s = v_s + TILE, *g_s = q_s + TILE, *pq_s = g_s + TILE, *pg_s = pq_s + C * C * 2, *r_s = pg_s + C * C * 2;
+    float *dots_q = (float*)(r_s + D * D * 2), *dots_g = dots_q + C, *powers_s = dots_g + C;
     int tid = threadIdx.x, l16 = tid & 15, quad = (tid >> 4) & 3;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -447,10 +464,9 @@ __global__ __launch_bounds__(D * 4, 2) void back_kernel(const Args args) {
     if (!place_of(args, args.spread, place)) return;
     const int u = place.u, kvh = place.kvh, sub = place.member, qh0 = kvh * args.ratio + sub * G;
     const User us = user_of(args, u);
-    const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK;
-    const bool full = args.full;
-    const Piece piece = piece_of(args, place.piece, nh, nt, true);
-    if (args.seg && piece.c0 >= piece.c1) return;
+    const Piece piece = piece_of(args, place.piece, us.L, us.T, true);
+    const int nt = (piece.t1 - piece.t0 + C - 1) / C, chunks = nt + (piece.h1 - piece.h0 + C - 1) / C;
+    if (args.seg && chunks == 0) return;
 
     State<D> R[G];
 #pragma unroll
@@ -462,48 +478,49 @@ __global__ __launch_bounds__(D * 4, 2) void back_kernel(const Args args) {
     const auto rows_of = [&](int c) {
         Rows r;
         r.hist = c >= nt;
-        const int first = (r.hist ? c - nt : c) * CHUNK, at = r.hist ? us.L - 1 - first : us.L + first;
-        r.n = min(CHUNK, (r.hist ? us.L : us.T) - first);
-        r.kv = us.kv0 + at, r.q = us.q0 + (full ? at : first);  // (q of a history's rows: only where they ask)
+        const int first = r.hist ? piece.h0 + (c - nt) * C : piece.t0 + c * C, at = r.hist ? us.L - 1 - first : us.L + first;
+        r.n = min(C, (r.hist ? piece.h1 : piece.t1) - first);
+        r.kv = us.kv0 + at, r.q = us.q0 + (FULL ? at : first);  // (q of a history's rows: only where they ask)
         return r;
     };
     const unsigned pitch_q = args.Hq * (D * 2), pitch_kv = args.Hkv * (D * 2);
     bf16x8 kw[LOADS], vw[LOADS], qw[LOADS], gw[LOADS];
     const auto fetch_kv = [&](int chunk) {
         const Rows r = rows_of(chunk);
-        const int64_t first = (lowest(r.hist, r.kv) * args.Hkv + kvh) * D;
+        const int64_t first = (lowest<C>(r.hist, r.kv) * args.Hkv + kvh) * D;
         const char *k = (const char*)(args.k + first), *v = (const char*)(args.v + first);
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
             const int row = tid / C16 + i * PART;
-            const unsigned at = bytes_of(r.hist, row, pitch_kv, tid % C16 * 16);
+            const unsigned at = bytes_of<C>(r.hist, row, pitch_kv, tid % C16 * 16);
             kw[i] = vw[i] = bf16x8{};
             if (row < r.n) kw[i] = *(const bf16x8*)(k + at), vw[i] = *(const bf16x8*)(v + at);
         }
     };
     const auto fetch_q = [&](int chunk, int g) {
         const Rows r = rows_of(chunk);
-        const int64_t first = (lowest(r.hist, r.q) * args.Hq + qh0 + g) * D;
+        const int64_t first = (lowest<C>(r.hist, r.q) * args.Hq + qh0 + g) * D;
         const char *q = (const char*)(args.q + first), *dout = (const char*)(args.dout + first);
-        const bool asks = full || !r.hist;
+        const bool asks = FULL || !r.hist;
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
             const int row = tid / C16 + i * PART;
-            const unsigned at = bytes_of(r.hist, row, pitch_q, tid % C16 * 16);
+            const unsigned at = bytes_of<C>(r.hist, row, pitch_q, tid % C16 * 16);
             qw[i] = gw[i] = bf16x8{};
             if (row < r.n && asks) qw[i] = *(const bf16x8*)(q + at), gw[i] = *(const bf16x8*)(dout + at);
         }
     };
-    if (piece.c0 < piece.c1) fetch_kv(piece.c0), fetch_q(piece.c0, 0);
+    if (chunks > 0) fetch_kv(0), fetch_q(0, 0);
     fill_powers<NT>(powers_s, args.log_decay + qh0, G, args.scale, tid);
-    for (int i = tid; i < 2 * CHUNK * CHUNK / 8; i += NT) lds<bf16x8>(pq_s, i * 16) = bf16x8{};
+    for (int i = tid; i < 2 * C * C / 8; i += NT) lds<bf16x8>(pq_s, i * 16) = bf16x8{};
     Lane<D> at(tid, l16, quad, wave);
-    Lane<CHUNK> at_p(0, l16, quad, 0);
+    Lane<C> at_p(0, l16, quad, 0);
 
-    floatx4 acc_v[4], acc_k[4];
-    for (int c = piece.c0; c < piece.c1; c++) {
+    floatx4 acc_v[IT], acc_k[IT];
+    const auto turn = [&](auto K, int c) {
+        constexpr Kind kind = decltype(K)::value;
+        constexpr bool hist = kind != CANDIDATES;
         const Rows r = rows_of(c);
-        const bool asks = full || !r.hist;
 #pragma unroll
         for (int g = 0; g < G; g++) {
             const float *power = powers_s + 2 * g * POWERS, *scaled = power + POWERS;
@@ -515,66 +532,79 @@ __global__ __launch_bounds__(D * 4, 2) void back_kernel(const Args args) {
                     lds<bf16x8>(k_s + i * PART * (D * 2), at.stage) = kw[i];
                     lds<bf16x8>(v_s + i * PART * (D * 2), at.stage) = vw[i];
                 }
-                lds<bf16x8>(q_s + i * PART * (D * 2), at.stage) = qw[i];
-                lds<bf16x8>(g_s + i * PART * (D * 2), at.stage) = gw[i];
+                if (kind != SILENT) {
+                    lds<bf16x8>(q_s + i * PART * (D * 2), at.stage) = qw[i];
+                    lds<bf16x8>(g_s + i * PART * (D * 2), at.stage) = gw[i];
+                }
             }
             bf16x8 s[KS];
-            if (r.hist) {  // R^T for the other waves: row 16 wave + l16 of it, 32 k + 8 quad .. + 7
+            if (hist) {  // R^T for the other waves: row 16 wave + l16 of it, 32 k + 8 quad .. + 7
                 R[g].rounded(s);
 #pragma unroll
                 for (int k = 0; k < KS; k++) lds<bf16x8>(r_s + wave * (16 * D * 2), at.row ^ (64 * k)) = s[k];
             }
             __syncthreads();
             if (g + 1 < G) fetch_q(c, g + 1);
-            else if (c + 1 < piece.c1) fetch_q(c + 1, 0);
-            if (g == G - 1 && c + 1 < piece.c1) fetch_kv(c + 1);
+            else if (c + 1 < chunks) fetch_q(c + 1, 0);
+            if (g == G - 1 && c + 1 < chunks) fetch_kv(c + 1);
 
-            if (r.hist && asks) {
+            if (kind == ASKING) {
 #pragma unroll
-                for (int t0 = 0; t0 < 20; t0 += NW) {
-                    const int t = t0 + wave, tt = t >= 10 ? t - 10 : t, it = tile_row(tt), jt = tt - it * (it + 1) / 2;
-                    if (t < 20) score_tile<D>(t >= 10 ? v_s : k_s, t >= 10 ? g_s : q_s, t >= 10 ? pg_s : pq_s, scaled, at, at_p, it, jt, l16, quad);
+                for (int t0 = 0; t0 < 2 * TILES; t0 += NW) {
+                    const int t = t0 + wave, tt = t >= TILES ? t - TILES : t, it = tile_row(tt), jt = tt - it * (it + 1) / 2;
+                    if (t0 + NW <= 2 * TILES || t < 2 * TILES)
+                        score_tile<D, C>(t >= TILES ? v_s : k_s, t >= TILES ? g_s : q_s, t >= TILES ? pg_s : pq_s, scaled, at, at_p, it, jt, l16, quad);
                 }
-            } else if (!r.hist) {
-                own_dots<D, NT>(k_s, q_s, dots_q, args.scale, tid);
-                own_dots<D, NT>(v_s, g_s, dots_g, args.scale, tid);
+            } else if (kind == CANDIDATES) {
+                own_dots<D, C, NT>(k_s, q_s, dots_q, args.scale, tid);
+                own_dots<D, C, NT>(v_s, g_s, dots_g, args.scale, tid);
             }
-            __syncthreads();
-            bf16x8 gt[2], qt[2];  // this wave's columns of dout and q, rows 32 k + 8 quad .. + 7
+            if (kind != SILENT) __syncthreads();
+            // dv, then dk: at most one of the two's operands in registers
+            const auto rows_of_out = [&](floatx4 (&acc)[IT], const bf16x8 (&ct)[KT], const bf16x8 (&state)[KS], char* p_tile, char* c_tile, char* a_tile, const float* dots) {
+                floatx4 x[IT];
+                if (kind == ASKING) within_chunk<D, C>(x, ct, p_tile, c_tile, at_p, wave, l16, quad);
 #pragma unroll
-            for (int k = 0; k < 2; k++) gt[k] = read_tr<D>(g_s + 32 * k * (D * 2), at.tr), qt[k] = read_tr<D>(q_s + 32 * k * (D * 2), at.tr);
-            bool odd_g = false, odd_q = false;
-            hta::static_for<0, 4>([&](auto I) {
-                constexpr int it = 3 - decltype(I)::value;
-                const int i = 16 * it + l16;
-                floatx4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-                if (!r.hist) {
-                    x = own_term<D>(dots_q, g_s, wave, i, quad), y = own_term<D>(dots_g, q_s, wave, i, quad);
-                } else {
-                    if (asks) {
-                        x = within_chunk<D, it>(gt, pq_s, g_s, at_p, wave, odd_g, l16, quad);
-                        y = within_chunk<D, it>(qt, pg_s, q_s, at_p, wave, odd_q, l16, quad);
+                for (int it = 0; it < IT; it++) {
+                    if (kind == CANDIDATES) x[it] = own_term<D>(dots, c_tile, wave, 16 * it + l16, quad);
+                    if (kind == SILENT) x[it] = floatx4{0.f, 0.f, 0.f, 0.f};
+                    if (hist) {
+                        floatx4 o;
+#pragma unroll
+                        for (int k = 0; k < KS; k++)
+                            o = mfma16(state[k], lds<bf16x8>(a_tile + it * (16 * D * 2), at.row ^ (64 * k)), k == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : o);
+                        const float f = power[ZERO + 16 * it + l16];
+#pragma unroll
+                        for (int v = 0; v < 4; v++) x[it][v] = fmaf(o[v], f, x[it][v]);
                     }
-                    floatx4 o = {0.f, 0.f, 0.f, 0.f}, p = o;
-#pragma unroll
-                    for (int k = 0; k < KS; k++) {
-                        o = mfma16(s[k], lds<bf16x8>(k_s + it * (16 * D * 2), at.row ^ (64 * k)), o);
-                        p = mfma16(read_tr<D>(r_s + 32 * k * (D * 2), at.tr), lds<bf16x8>(v_s + it * (16 * D * 2), at.row ^ (64 * k)), p);
-                    }
-                    const float f = power[ZERO + i];
-#pragma unroll
-                    for (int v = 0; v < 4; v++) x[v] = fmaf(o[v], f, x[v]), y[v] = fmaf(p[v], f, y[v]);
+                    acc[it] = g == 0 ? x[it] : acc[it] + x[it];
+                    asm volatile("" : "+v"(acc[it]));  // (formed here: left to the compiler, it is formed where it is used next, from operands that stay until then)
                 }
-                acc_v[it] = g == 0 ? x : acc_v[it] + x;
-                acc_k[it] = g == 0 ? y : acc_k[it] + y;
-            });
-            if (g == G - 1) {
-                const int64_t base = (lowest(r.hist, r.kv) * args.Hkv + kvh) * D, slab = (int64_t)sub * args.total_kv * args.Hkv * D;
+            };
+            bf16x8 gt[KT];  // this wave's columns of dout, rows 32 k + 8 quad .. + 7
+            if (kind != SILENT)
 #pragma unroll
-                for (int it = 0; it < 4; it++) {
+                for (int k = 0; k < KT; k++) gt[k] = read_tr<D>(g_s + 32 * k * (D * 2), at.tr);
+            rows_of_out(acc_v, gt, s, pq_s, g_s, k_s, dots_q);
+            __builtin_amdgcn_sched_barrier(0);
+            {
+                bf16x8 qt[KT], st[KS];  // this wave's columns of q; its rows of R^T
+                if (kind != SILENT)
+#pragma unroll
+                    for (int k = 0; k < KT; k++) qt[k] = read_tr<D>(q_s + 32 * k * (D * 2), at.tr);
+                if (hist)
+#pragma unroll
+                    for (int k = 0; k < KS; k++) st[k] = read_tr<D>(r_s + 32 * k * (D * 2), at.tr);
+                rows_of_out(acc_k, qt, st, pg_s, q_s, v_s, dots_g);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (g == G - 1) {
+                const int64_t base = (lowest<C>(hist, r.kv) * args.Hkv + kvh) * D, slab = (int64_t)sub * args.total_kv * args.Hkv * D;
+#pragma unroll
+                for (int it = 0; it < IT; it++) {
                     const int i = 16 * it + l16;
                     if (i >= r.n) continue;
-                    const unsigned to = bytes_of(r.hist, i, pitch_kv, 32 * wave + 8 * quad);
+                    const unsigned to = bytes_of<C>(hist, i, pitch_kv, 32 * wave + 8 * quad);
                     if (args.partial_k) {
                         *(floatx4*)((char*)(args.partial_v + slab + base) + 2 * to) = acc_v[it];
                         *(floatx4*)((char*)(args.partial_k + slab + base) + 2 * to) = acc_k[it];
@@ -587,68 +617,66 @@ __global__ __launch_bounds__(D * 4, 2) void back_kernel(const Args args) {
                     }
                 }
             }
-            if (r.hist) R[g].keep(power[ZERO + r.n]);
-            if (asks) R[g].add(q_s, gt, scaled + ZERO + (r.hist ? r.n : 1), r.hist ? 1 : 0, at, quad);
+            if (hist) R[g].keep(power[ZERO + r.n]);
+            if (kind != SILENT) R[g].add(q_s, gt, scaled + ZERO + (hist ? r.n : 1), std::integral_constant<int, hist ? 1 : 0>{}, at, quad, args.state_out != nullptr);
             __syncthreads();
         }
-    }
+    };
+    int c = 0;
+    for (; c < nt; c++) turn(KindOf<CANDIDATES>{}, c);
+    for (; c < chunks; c++) turn(KindOf<FULL ? ASKING : SILENT>{}, c);
     if (args.state_out && !args.seg)
 #pragma unroll
         for (int g = 0; g < G; g++) R[g].store(args.state_out + ((int64_t)u * args.Hq + qh0 + g) * D * D, wave, l16, quad);
 }
-template <int D, int G>
-constexpr int back_lds() { return 4 * CHUNK * D * 2 + 2 * CHUNK * CHUNK * 2 + D * D * 2 + (2 * CHUNK + 2 * G * POWERS) * 4; }
+template <int D, int G, int C>
+constexpr int back_lds() { return 4 * C * D * 2 + 2 * C * C * 2 + D * D * 2 + (2 * C + 2 * G * POWERS) * 4; }
 
 // What each piece adds to a state that starts at zero: forwards sum_j l^(n-1-j) b_j c_j^T over a history's piece, backwards scale times sum_j l^(n-j) q_j dout_j^T
 // over either kind (candidates: l).  blockIdx.y: 1 backwards.
-template <int D>
-__global__ __launch_bounds__(D * 4, 4) void states_kernel(const Args args, int first_job) {
-    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, PART = NT / C16, LOADS = CHUNK / PART, TILE = CHUNK * D * 2;
+template <int D, int C>
+__global__ __launch_bounds__(D * 4, 4) void states_kernel(const Args args, int first_job, int whole_jobs) {
+    constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, PART = NT / C16, LOADS = C / PART, TILE = C * D * 2, KT = C / 32;
     __shared__ __attribute__((aligned(16))) char b_s[TILE], c_s[TILE];
     __shared__ float powers_s[2 * POWERS];
     int tid = threadIdx.x, l16 = tid & 15, quad = (tid >> 4) & 3;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const bool back = (int)blockIdx.y + first_job == 1;
+    const bool back = (int)blockIdx.y + first_job == 1, whole = whole_jobs & (back ? 2 : 1);
 
     Place place;
     if (!place_of(args, args.ratio, place)) return;
     const int u = place.u, kvh = place.kvh, qh = kvh * args.ratio + place.member;
     const User us = user_of(args, u);
-    const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK;
-    const Piece piece = piece_of(args, place.piece, nh, nt, back);
-    if (piece.c0 >= piece.c1 || (back ? piece.hist && !args.full : !piece.hist)) return;
+    const Piece piece = piece_of(args, place.piece, us.L, us.T, back);
+    const bool hist = piece.h1 > piece.h0;
+    const int from = hist ? piece.h0 : piece.t0, rows = hist ? piece.h1 - piece.h0 : piece.t1 - piece.t0, chunks = (rows + C - 1) / C;
+    if (chunks == 0 || (back ? hist && !args.full : !hist)) return;
 
     const int heads = back ? args.Hq : args.Hkv, head = back ? qh : kvh;
     const unsigned pitch = heads * (D * 2);
     const __bf16 *bg = back ? args.q : args.b, *cg = back ? args.dout : args.c;
     bf16x8 bv[LOADS], cv[LOADS];
-    const auto rows_left = [&](int c) {  // (of the chunk: its rows, and the first one)
-        const int first = (piece.hist ? (back ? c - nt : c) : back ? c : c - nh) * CHUNK;
-        const int64_t at = !back ? us.kv0 + first : us.q0 + (piece.hist ? us.L - 1 - first : (args.full ? us.L : 0) + first);
-        struct { int n; int64_t at; } r = {min(CHUNK, (piece.hist ? us.L : us.T) - first), at};
-        return r;
-    };
-    const bool down = back && piece.hist;
+    const bool down = back && hist;
     const auto fetch = [&](int c) {
-        const auto r = rows_left(c);
-        const int64_t first = (lowest(down, r.at) * heads + head) * D;
+        const int at0 = from + c * C, n = min(C, rows - c * C);
+        const int64_t row0 = !back ? us.kv0 + at0 : us.q0 + (hist ? us.L - 1 - at0 : (args.full ? us.L : 0) + at0), first = (lowest<C>(down, row0) * heads + head) * D;
         const char *b = (const char*)(bg + first), *x = (const char*)(cg + first);
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
             const int row = tid / C16 + i * PART;
-            const unsigned at = bytes_of(down, row, pitch, tid % C16 * 16);
+            const unsigned at = bytes_of<C>(down, row, pitch, tid % C16 * 16);
             bv[i] = cv[i] = bf16x8{};
-            if (row < r.n) bv[i] = *(const bf16x8*)(b + at), cv[i] = *(const bf16x8*)(x + at);
+            if (row < n) bv[i] = *(const bf16x8*)(b + at), cv[i] = *(const bf16x8*)(x + at);
         }
     };
-    fetch(piece.c0);
+    fetch(0);
     fill_powers<NT>(powers_s, args.log_decay + qh, 1, args.scale, tid);
     const float *power = powers_s, *scaled = powers_s + POWERS;
     Lane<D> at(tid, l16, quad, wave);
     State<D> S;
     S.zero();
-    for (int c = piece.c0; c < piece.c1; c++) {
-        const int n = rows_left(c).n;
+    for (int c = 0; c < chunks; c++) {
+        const int n = min(C, rows - c * C);
         at.forget(tid, l16, quad);
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
@@ -656,12 +684,13 @@ __global__ __launch_bounds__(D * 4, 4) void states_kernel(const Args args, int f
             lds<bf16x8>(c_s + i * PART * (D * 2), at.stage) = cv[i];
         }
         __syncthreads();
-        if (c + 1 < piece.c1) fetch(c + 1);
-        bf16x8 ct[2];
+        if (c + 1 < chunks) fetch(c + 1);
+        bf16x8 ct[KT];
 #pragma unroll
-        for (int k = 0; k < 2; k++) ct[k] = read_tr<D>(c_s + 32 * k * (D * 2), at.tr);
-        if (piece.hist) S.keep(power[ZERO + n]);
-        S.add(b_s, ct, back ? scaled + ZERO + (piece.hist ? n : 1) : power + ZERO + n - 1, piece.hist ? 1 : 0, at, quad);
+        for (int k = 0; k < KT; k++) ct[k] = read_tr<D>(c_s + 32 * k * (D * 2), at.tr);
+        if (hist) S.keep(power[ZERO + n]);
+        if (hist) S.add(b_s, ct, back ? scaled + ZERO + n : power + ZERO + n - 1, std::integral_constant<int, 1>{}, at, quad, whole);
+        else S.add(b_s, ct, scaled + ZERO + 1, std::integral_constant<int, 0>{}, at, quad, whole);
         __syncthreads();
     }
     S.store((back ? args.states_back : args.states) + state_index(args, u, qh, piece.state) * D * D, wave, l16, quad);
@@ -675,8 +704,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const Args args, int
     const bool back = (int)blockIdx.z + first_job == 1;
     const int u = blockIdx.x / args.Hq, h = blockIdx.x % args.Hq, e = (blockIdx.y * SCAN_THREADS + threadIdx.x) * 4;
     const User us = user_of(args, u);
-    const int nh = (us.L + CHUNK - 1) / CHUNK, nt = (us.T + CHUNK - 1) / CHUNK, seg = args.seg, rows = seg * CHUNK;
-    const int hs = (nh + seg - 1) / seg, ts = back ? (nt + seg - 1) / seg : 0, n = hs + ts;
+    const int rows = args.seg, hs = (us.L + rows - 1) / rows, ts = back ? (us.T + rows - 1) / rows : 0, n = hs + ts;
     const float g2 = fmaxf(fminf(args.log_decay[h], 0.f) * hta::LOG2E, MIN_LOG2), all = fast_exp2(g2 * (float)rows);
     const float last = fast_exp2(g2 * (float)(us.L - (hs - 1) * rows));
     const int64_t state = ((int64_t)u * args.Hq + h) * D * D;
@@ -708,7 +736,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const Args args, int
 }
 
 // dk, dv = the sum of a group's shares, for the rows of the users
-constexpr int SUM_THREADS = 256, SUM_BLOCKS = 16;  // (per user)
+constexpr int SUM_THREADS = 256, SUM_BLOCKS = 64;  // (per user)
 __global__ __launch_bounds__(SUM_THREADS) void sum_kernel(const Args args, int d) {
     const User us = user_of(args, blockIdx.x);
     const float* partial = blockIdx.z ? args.partial_k : args.partial_v;
@@ -819,8 +847,13 @@ int check_sizes(int layer, int dtype, int32_t batch, int64_t total_q, int64_t to
     return MTFM_HTA_OK;
 }
 
-constexpr int MIN_SEG = 4;  // chunks of a piece at least
+constexpr int ORDER_RATIO = 2;
+constexpr int MIN_SEG = 256;  // rows of a piece at least; a multiple of what a chunk has
 constexpr int PER_CU(int d) { return d == 128 ? 2 : 4; }  // workgroups that a compute unit holds
+
+// rows of a chunk
+constexpr int sweep_rows(int D) { return D == 128 ? 32 : 64; }
+constexpr int BACK_ROWS = 64, STATES_ROWS = 32;
 
 // heads of a group that a backward workgroup holds: what registers allow of the largest power of two that divides the group
 int heads_per_workgroup(int ratio, int d) {
@@ -835,6 +868,8 @@ struct Plan {
     size_t partial;     // bytes of dk's (dv's) shares, 0 for none
     int seg, n_hist, n_tgt;
     size_t states;      // bytes of the pieces' states, one direction
+    size_t order;       // bytes of the users' order, 0: as they come
+    size_t bytes(bool backward) const { return order + 2 * partial + (backward ? 2 : 1) * states; }
 };
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
@@ -846,14 +881,26 @@ Plan plan_of(bool backward, int batch, int64_t total_kv, int max_hist, int max_t
     // Pieces: where users' heads do not fill the chip, a user's history is cut until they do.
     const int places = 256 * PER_CU(d);
     const int64_t whole = (int64_t)batch * Hq;
-    const int chunks = ceil_div(max_hist, CHUNK);
     const int64_t cuts = places / whole;
-    if (cuts >= 2 && chunks >= 2 * MIN_SEG) {
-        p.seg = ceil_div(chunks, cuts) < MIN_SEG ? MIN_SEG : ceil_div(chunks, cuts);
-        p.n_hist = ceil_div(chunks, p.seg), p.n_tgt = ceil_div(ceil_div(max_targets, CHUNK), p.seg);
+    if (cuts >= 2 && max_hist >= 2 * MIN_SEG) {
+        p.seg = ceil_div(ceil_div(max_hist, cuts), MOST_ROWS) * MOST_ROWS;
+        if (p.seg < MIN_SEG) p.seg = MIN_SEG;
+        p.n_hist = ceil_div(max_hist, p.seg), p.n_tgt = ceil_div(max_targets, p.seg);
         p.states = align256((size_t)whole * (p.n_hist + p.n_tgt + 1) * d * d * sizeof(float));
     }
+    // Long users first, where lengths differ and there are more of them than places: the last ones to start are short.  (A launch of 4 us.)
+    const bool even = (double)total_kv >= 0.9 * (double)batch * ((double)max_hist + max_targets);
+    if (!p.seg && !even && whole * ORDER_RATIO > places && max_hist > MIN_SEG) p.order = align256(hta::schedule_bytes(batch));
     return p;
+}
+
+// the head of the workspace: the users' order
+hipError_t launch_order(Args& a, const Plan& plan, void* workspace, hipStream_t s) {
+    if (!plan.order) return hipSuccess;
+    hta::Params p = {};
+    p.hist_len = a.hist_len, p.n_targets = a.n_targets, p.batch = a.batch, p.max_hist = a.max_hist, p.max_targets = a.max_targets;
+    a.order = hta::schedule_order(workspace);
+    return hta::launch_schedule(p, workspace, s);
 }
 
 int64_t grid_of(const Args& a, int members) {
@@ -863,7 +910,9 @@ int64_t grid_of(const Args& a, int members) {
 
 template <int D>
 hipError_t launch_sweep_d(const Args& a, hipStream_t s) {
-    hipLaunchKernelGGL((sweep_kernel<D>), dim3((unsigned)grid_of(a, a.ratio)), dim3(D * 4), 0, s, a);
+    const dim3 grid((unsigned)grid_of(a, a.ratio));
+    if (a.full) hipLaunchKernelGGL((sweep_kernel<D, sweep_rows(D), true>), grid, dim3(D * 4), 0, s, a);
+    else hipLaunchKernelGGL((sweep_kernel<D, sweep_rows(D), false>), grid, dim3(D * 4), 0, s, a);
     return hipGetLastError();
 }
 hipError_t launch_sweep(const Args& a, int d, hipStream_t s) {
@@ -873,7 +922,7 @@ hipError_t launch_sweep(const Args& a, int d, hipStream_t s) {
 // first_job, jobs: 0, 1 the sweep in the tokens' order; 1, 1 backwards; 0, 2 both
 template <int D>
 hipError_t launch_states_d(const Args& a, int first_job, int jobs, const float* in_ahead, float* out_ahead, const float* in_back, float* out_back, hipStream_t s) {
-    hipLaunchKernelGGL((states_kernel<D>), dim3((unsigned)grid_of(a, a.ratio), jobs), dim3(D * 4), 0, s, a, first_job);
+    hipLaunchKernelGGL((states_kernel<D, STATES_ROWS>), dim3((unsigned)grid_of(a, a.ratio), jobs), dim3(D * 4), 0, s, a, first_job, (out_ahead ? 1 : 0) | (out_back ? 2 : 0));
     hipLaunchKernelGGL((scan_kernel<D>), dim3(a.batch * a.Hq, D * D / (SCAN_THREADS * 4), jobs), dim3(SCAN_THREADS), 0, s, a, first_job, in_ahead, a.transposed,
                        out_ahead, in_back, out_back);
     return hipGetLastError();
@@ -892,16 +941,21 @@ hipError_t allow_lds(int bytes) {
     static hipError_t state = hipFuncSetAttribute((const void*)Kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     return state;
 }
-template <int D, int G>
+template <int D, int G, bool FULL>
 hipError_t launch_back_as(const Args& a, hipStream_t s) {
-    constexpr int lds = back_lds<D, G>();
-    if (hipError_t e = allow_lds<back_kernel<D, G>>(lds); e != hipSuccess) return e;
-    hipLaunchKernelGGL((back_kernel<D, G>), dim3((unsigned)grid_of(a, a.spread)), dim3(D * 4), lds, s, a);
+    constexpr int C = BACK_ROWS, lds = back_lds<D, G, C>();
+    if (hipError_t e = allow_lds<back_kernel<D, G, C, FULL>>(lds); e != hipSuccess) return e;
+    hipLaunchKernelGGL((back_kernel<D, G, C, FULL>), dim3((unsigned)grid_of(a, a.spread)), dim3(D * 4), lds, s, a);
     return hipGetLastError();
 }
+template <int D, int G>
+hipError_t launch_back_layer(const Args& a, hipStream_t s) { return a.full ? launch_back_as<D, G, true>(a, s) : launch_back_as<D, G, false>(a, s); }
 template <int D>
 hipError_t launch_back_d(const Args& a, int G, hipStream_t s) {
-    return G == 1 ? launch_back_as<D, 1>(a, s) : G == 2 ? launch_back_as<D, 2>(a, s) : launch_back_as<D, 4>(a, s);
+    if (G == 1) return launch_back_layer<D, 1>(a, s);
+    if (G == 2) return launch_back_layer<D, 2>(a, s);
+    if constexpr (D < 128) return launch_back_layer<D, 4>(a, s);
+    return hipErrorInvalidValue;
 }
 hipError_t launch_back(const Args& a, int d, int G, hipStream_t s) {
     return d == 32 ? launch_back_d<32>(a, G, s) : d == 64 ? launch_back_d<64>(a, G, s) : launch_back_d<128>(a, G, s);
@@ -960,7 +1014,7 @@ size_t mtfm_hla_workspace_bytes(int layer, int dtype, int is_bwd, int32_t batch,
     if (hla::check_sizes(layer, dtype, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, head_dim) != MTFM_HTA_OK) return (size_t)-1;
     if (batch == 0) return 0;
     const hla::Plan plan = hla::plan_of(is_bwd, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
-    return 2 * plan.partial + (is_bwd ? 2 : 1) * plan.states;
+    return plan.bytes(is_bwd);
 }
 
 int mtfm_hla_fwd(const void* q, const void* k, const void* v, const float* log_decay, const float* state, void* out, float* final_state,
@@ -971,13 +1025,13 @@ int mtfm_hla_fwd(const void* q, const void* k, const void* v, const float* log_d
     if (batch == 0) return MTFM_HTA_OK;
     if (int rc = hla::check_arrays({q, out}, {k, v}, {state, final_state}, log_decay, {q_offsets, kv_offsets, hist_len, n_targets}, total_q, total_kv, scale)) return rc;
     const hla::Plan plan = hla::plan_of(false, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
-    if (int rc = hla::check_workspace(plan.states, workspace, workspace_bytes)) return rc;
+    if (int rc = hla::check_workspace(plan.bytes(false), workspace, workspace_bytes)) return rc;
     hla::Args a = hla::args_of(log_decay, q_offsets, kv_offsets, hist_len, n_targets, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, scale, layer);
-    a.seg = plan.seg, a.n_hist = plan.n_hist, a.n_tgt = plan.n_tgt, a.states = (float*)workspace;
+    a.seg = plan.seg, a.n_hist = plan.n_hist, a.n_tgt = plan.n_tgt, a.states = (float*)((char*)workspace + plan.order);
     a.a = (const __bf16*)q, a.b = (const __bf16*)k, a.c = (const __bf16*)v, a.out = (__bf16*)out, a.state_in = state, a.state_out = final_state;
     hipStream_t s = (hipStream_t)stream;
-    hipError_t e = hipSuccess;
-    if (plan.seg) e = hla::launch_states(a, head_dim, 0, 1, state, final_state, nullptr, nullptr, s);
+    hipError_t e = hla::launch_order(a, plan, workspace, s);
+    if (e == hipSuccess && plan.seg) e = hla::launch_states(a, head_dim, 0, 1, state, final_state, nullptr, nullptr, s);
     if (e == hipSuccess && (total_q > 0 || !plan.seg)) {
         hta::timing_begin(MTFM_HLA_KERNEL_FWD, s);
         e = hla::launch_sweep(a, head_dim, s);
@@ -997,15 +1051,15 @@ int mtfm_hla_bwd(const void* dout, const void* q, const void* k, const void* v, 
                                    total_kv, scale))
         return rc;
     const hla::Plan plan = hla::plan_of(true, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
-    if (int rc = hla::check_workspace(2 * plan.partial + 2 * plan.states, workspace, workspace_bytes)) return rc;
+    if (int rc = hla::check_workspace(plan.bytes(true), workspace, workspace_bytes)) return rc;
     hla::Args a = hla::args_of(log_decay, q_offsets, kv_offsets, hist_len, n_targets, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, scale, layer);
     hipStream_t s = (hipStream_t)stream;
     const auto Q = (const __bf16*)q, K = (const __bf16*)k, V = (const __bf16*)v, dO = (const __bf16*)dout;
-    hipError_t e = hipSuccess;
+    hipError_t e = hla::launch_order(a, plan, workspace, s);
     a.q = Q, a.k = K, a.v = V, a.dout = dO, a.dk = (__bf16*)dk, a.dv = (__bf16*)dv, a.b = V, a.c = K, a.transposed = 1;
     a.seg = plan.seg, a.n_hist = plan.n_hist, a.n_tgt = plan.n_tgt;
-    a.states = (float*)((char*)workspace + 2 * plan.partial), a.states_back = a.states + plan.states / sizeof(float);
-    if (plan.seg) e = hla::launch_states(a, head_dim, total_q > 0 ? 0 : 1, total_q > 0 ? 2 : 1, state, nullptr, dfinal_state, dstate, s);
+    a.states = (float*)((char*)workspace + plan.order + 2 * plan.partial), a.states_back = a.states + plan.states / sizeof(float);
+    if (e == hipSuccess && plan.seg) e = hla::launch_states(a, head_dim, total_q > 0 ? 0 : 1, total_q > 0 ? 2 : 1, state, nullptr, dfinal_state, dstate, s);
     hta::timing_begin(MTFM_HLA_KERNEL_BWD, s);
     if (e == hipSuccess && total_q > 0) {
         a.a = dO, a.out = (__bf16*)dq, a.state_in = state;
@@ -1013,7 +1067,7 @@ int mtfm_hla_bwd(const void* dout, const void* q, const void* k, const void* v, 
     }
     if (e == hipSuccess) {
         a.state_in = dfinal_state, a.state_out = dstate, a.spread = plan.spread;
-        if (plan.spread > 1) a.partial_k = (float*)workspace, a.partial_v = a.partial_k + plan.partial / sizeof(float);
+        if (plan.spread > 1) a.partial_k = (float*)((char*)workspace + plan.order), a.partial_v = a.partial_k + plan.partial / sizeof(float);
         e = hla::launch_back(a, head_dim, plan.G, s);
     }
     hta::timing_end(MTFM_HLA_KERNEL_BWD, s);
