@@ -719,12 +719,13 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const Args args, int
         else x = *(const floatx4*)(in + state + e);
     }
     const bool adds = args.full || !back;  // (backwards through a history that does not ask nothing is added)
-    for (int s = 0; s < n; s += 4) {
-        floatx4 y[4];
+    constexpr int AHEAD = 16;  // loads in flight: the sum is all latency
+    for (int s = 0; s < n; s += AHEAD) {
+        floatx4 y[AHEAD];
 #pragma unroll
-        for (int i = 0; i < 4; i++) y[i] = s + i < n && (adds || s + i < ts) ? *(const floatx4*)(p + (int64_t)(s + i) * D * D) : floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < AHEAD; i++) y[i] = s + i < n && (adds || s + i < ts) ? *(const floatx4*)(p + (int64_t)(s + i) * D * D) : floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
+        for (int i = 0; i < AHEAD; i++) {
             if (s + i >= n) break;
             const float f = s + i < ts ? 1.f : s + i == n - 1 ? last : all;
             *(floatx4*)(p + (int64_t)(s + i) * D * D) = x;
@@ -881,7 +882,7 @@ Plan plan_of(bool backward, int batch, int64_t total_kv, int max_hist, int max_t
     // Pieces: where users' heads do not fill the chip, a user's history is cut until they do.
     const int places = 256 * PER_CU(d);
     const int64_t whole = (int64_t)batch * Hq;
-    const int64_t cuts = places / whole;
+    const int64_t cuts = places / whole - 1;  // (and a piece for the candidates)
     if (cuts >= 2 && max_hist >= 2 * MIN_SEG) {
         p.seg = ceil_div(ceil_div(max_hist, cuts), MOST_ROWS) * MOST_ROWS;
         if (p.seg < MIN_SEG) p.seg = MIN_SEG;

@@ -101,11 +101,12 @@ class DecayBatch:
         back = dout is not None
         P = hta._address
         grads = (dout.data_ptr(), self.dq.data_ptr(), self.dk.data_ptr(), self.dv.data_ptr(), P(dfinal), P(self.dstate)) if back else (0,) * 6
-        lib = _declared or load_library()
-        status = lib.mtfm_binding_hla(_BLOCK.pack(
+        q_offsets, kv_offsets, hist_len, n_targets = self.ints
+        status = (_declared or load_library()).mtfm_binding_hla(_BLOCK.pack(
             self.q.data_ptr(), self.k.data_ptr(), self.v.data_ptr(), self.out.data_ptr(), self.log_decay.data_ptr(), P(self.state),
-            P(self.final_state), *grads, *(t.data_ptr() for t in self.ints), P(workspace), 0 if workspace is None else workspace.numel(),
-            self.total_q, self.total_kv, *self.sizes, self.scale, hta.BF16, self.layer, back), hta._stream_handle(stream))
+            P(self.final_state), *grads, q_offsets.data_ptr(), kv_offsets.data_ptr(), hist_len.data_ptr(), n_targets.data_ptr(), P(workspace),
+            0 if workspace is None else workspace.numel(), self.total_q, self.total_kv, *self.sizes, self.scale, hta.BF16, self.layer, back),
+            hta._stream_handle(stream))
         if status != hta.OK:
             raise hta.HtaError(status, hta.mtfm_hta_last_error())
 
@@ -138,28 +139,31 @@ def mtfm_hla_step(q, k, v, state, slots, log_decay, scale, new_state=None, out=N
     """One history token per row: q [rows, Hq, d], k, v [rows, Hkv, d]; row i's state is slot slots[i] (int32; None: i) of the pool
     `state` [slots, Hq, d, d] float32, and what follows goes to the same slot of `new_state` (None: in place).  Rows of one slot are
     tokens in the order of the rows; a row whose slot is not in the pool is padding, with output zero.  Returns out like q."""
-    _check_tokens(q, k, v)
-    rows, Hq, d = q.shape
-    if k.shape[0] != rows:
-        raise ValueError(f"{rows} rows of q, {k.shape[0]} of k")
-    if state.dim() != 4:
-        raise ValueError(f"state: [slots, Hq, head_dim, head_dim] expected, got {tuple(state.shape)}")
-    _check("state", state, (state.shape[0], Hq, d, d), torch.float32)
+    # (one condition for all that is right: a call is worth a few microseconds, and each look at a tensor a tenth of one; what is wrong is said by _check)
+    qs, ks, ss, bf16, f32 = q.shape, k.shape, state.shape, torch.bfloat16, torch.float32
+    if not (len(qs) == 3 and len(ks) == 3 and ks[0] == qs[0] and ks[2] == qs[2] and len(ss) == 4 and ss[1] == qs[1] and ss[2] == ss[3] == qs[2]
+            and v.shape == ks and q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and state.dtype is f32
+            and q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and state.is_contiguous()):
+        _check_tokens(q, k, v)
+        _check("k", k, (qs[0], *ks[1:]), bf16)
+        _check("state", state, (*ss[:1], *qs[1:], qs[2]), f32)
+    rows, Hq, d = qs
     if new_state is None:
         new_state = state
-    else:
-        _check("new_state", new_state, state.shape, torch.float32)
-    if slots is not None:
+    elif new_state.shape != ss or new_state.dtype is not f32 or not new_state.is_contiguous():
+        _check("new_state", new_state, ss, f32)
+    if slots is not None and (slots.dim() != 1 or slots.shape[0] != rows or slots.dtype is not torch.int32 or not slots.is_contiguous()):
         _check("slots", slots, (rows,), torch.int32)
-    _check("log_decay", log_decay, (Hq,), torch.float32)
+    if log_decay.dim() != 1 or log_decay.shape[0] != Hq or log_decay.dtype is not f32 or not log_decay.is_contiguous():
+        _check("log_decay", log_decay, (Hq,), f32)
     if out is None:
         out = torch.empty_like(q)
     else:
-        _check("out", out, q.shape, torch.bfloat16)
+        _check("out", out, qs, bf16)
     hta.check_on_current_device(q, k, v, state, slots, log_decay, new_state, out)
     status = (_declared or load_library()).mtfm_binding_hla_step(_STEP_BLOCK.pack(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state.data_ptr(), new_state.data_ptr(), hta._address(slots),
-        out.data_ptr(), rows, state.shape[0], Hq, k.shape[1], d, scale, hta.BF16, 0), hta._stream_handle(stream))
+        out.data_ptr(), rows, ss[0], Hq, ks[1], d, scale, hta.BF16, 0), hta._stream_handle(stream))
     if status != hta.OK:
         raise hta.HtaError(status, hta.mtfm_hta_last_error())
     return out

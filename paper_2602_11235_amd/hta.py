@@ -96,13 +96,13 @@ _device_index = getattr(torch._C, "_cuda_getDevice", None)
 
 def check_on_current_device(*tensors) -> None:
     """Kernels run on the current GPU, and so must all tensors (None: one that is not there) lie."""
-    for t in tensors:
-        if t is not None and t.get_device() < 0:
-            raise ValueError(f"all tensors must be on the current GPU, got one on {t.device}")
-    here = torch.cuda.current_device() if _device_index is None else _device_index()
+    try:
+        here = torch.cuda.current_device() if _device_index is None else _device_index()
+    except RuntimeError:  # no GPU at all
+        here = None
     for t in tensors:
         if t is not None and t.get_device() != here:
-            raise ValueError(f"all tensors must be on the current GPU ({here}), got one on {t.device}")
+            raise ValueError(f"all tensors must be on the current GPU{'' if here is None else f' ({here})'}, got one on {t.device}")
 
 
 def _current_stream() -> int:

@@ -50,35 +50,38 @@ def _call(fields) -> None:
         raise hta.HtaError(status, hta.mtfm_hta_last_error())
 
 
-def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.bfloat16:
-        return hta.BF16
-    if t.dtype == torch.float32:
-        return hta.FP32
-    raise TypeError(f"unsupported element type {t.dtype}")
+_CODES = {torch.bfloat16: hta.BF16, torch.float32: hta.FP32}
 
 
-def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None) -> int:
+def _operand(x: torch.Tensor):
+    """(shape, element type, its code) of the operand that the others are like."""
+    if x.dim() != 2:
+        raise ValueError(f"[rows, width] expected, got {tuple(x.shape)}")
+    code = _CODES.get(x.dtype)
+    if code is None:
+        raise TypeError(f"unsupported element type {x.dtype}")
+    return x.shape, x.dtype, code
+
+
+def _rows(name: str, t: torch.Tensor, shape, dtype) -> int:
     """Row stride of an operand [rows, width] whose rows are contiguous."""
-    if t.dim() != 2 or (like is not None and (t.shape != like.shape or t.dtype != like.dtype)):
-        raise ValueError(f"{name}: [rows, width]{'' if like is None else ' like the others'} expected, got {tuple(t.shape)} {t.dtype}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name}: {tuple(shape)} {dtype} expected, got {tuple(t.shape)} {t.dtype}")
+    if t.is_contiguous():
+        return shape[1]
+    if t.stride(1) != 1:
         raise ValueError(f"{name}: rows must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.stride(0)
 
 
 def _vector(name: str, t: torch.Tensor, n: int) -> None:
-    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+    if t.dtype is not torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         raise ValueError(f"{name}: {n} contiguous float32 values expected, got {tuple(t.shape)} {t.dtype}")
 
 
-def _out(name: str, t: Optional[torch.Tensor], like: torch.Tensor, dtype=None) -> torch.Tensor:
-    """An output [rows, width]: the given one, or a new one."""
-    dtype = dtype or like.dtype
-    if t is None:
-        return torch.empty(like.shape, dtype=dtype, device=like.device)
-    if t.shape != like.shape or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous {tuple(like.shape)} {dtype} expected, got {tuple(t.shape)} {t.dtype}")
+def _out(name: str, t: torch.Tensor, shape, dtype) -> torch.Tensor:
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {tuple(shape)} {dtype} expected, got {tuple(t.shape)} {t.dtype}")
     return t
 
 
@@ -86,17 +89,18 @@ def mtfm_rms_bwd_workspace_bytes(width: int) -> int:
     return int(load_library().mtfm_rms_bwd_workspace_bytes(width))
 
 
-def _forward(call, x, weight, eps, residual, h, y, rstd, scale, kind):
-    n, d = x.shape
-    code, x_stride, r_stride = _dtype_code(x), _rows("x", x), 0
+def _forward(call, x, weight, eps, residual, h, y, rstd, scale, kind, operand):
+    shape, dtype, code = operand
+    n, d = shape
+    x_stride, r_stride = _rows("x", x, shape, dtype), 0
     _vector("weight", weight, d)
+    P = hta._address
     if residual is not None:
-        r_stride = _rows("residual", residual, x)
-        h = _out("h", h, x)
+        r_stride = _rows("residual", residual, shape, dtype)
+        h = torch.empty_like(x, memory_format=torch.contiguous_format) if h is None else _out("h", h, shape, dtype)
     elif h is not None:
         raise ValueError("h without a residual is x")
     hta.check_on_current_device(x, weight, residual, h, y, rstd, scale)
-    P = hta._address
     _call((x.data_ptr(), P(residual), weight.data_ptr(), P(h), y.data_ptr(), P(rstd), P(scale), 0, 0, 0, x_stride, r_stride, 0, n, 0,
            d, eps, code, kind, call))
     return x if h is None else h
@@ -108,13 +112,14 @@ def mtfm_rms_fwd(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
     """(y, h, rstd) of rows x [n, width] (bf16 or float32) and weight [width] (float32).  h is the sum with the residual (x itself
     without one) and with rstd what the backward pass reads; rstd is None when save_rstd is False.  Outputs may be given, and may
     be the inputs' own memory (y is x, h is residual)."""
-    _rows("x", x)
-    y = _out("y", y, x)
+    operand = _operand(x)
+    shape, dtype, _ = operand
+    y = torch.empty_like(x, memory_format=torch.contiguous_format) if y is None else _out("y", y, shape, dtype)
     if rstd is not None:
-        _vector("rstd", rstd, x.shape[0])
+        _vector("rstd", rstd, shape[0])
     elif save_rstd:
-        rstd = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    return y, _forward(_FWD, x, weight, eps, residual, h, y, rstd, None, 0), rstd
+        rstd = weight.new_empty(shape[0])
+    return y, _forward(_FWD, x, weight, eps, residual, h, y, rstd, None, 0, operand), rstd
 
 
 def mtfm_rms_fwd_q8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
@@ -123,32 +128,33 @@ def mtfm_rms_fwd_q8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual:
     """(q, scale, h) with y = q * scale[:, None] in 8 bits, `kind` torch.int8 or torch.float8_e4m3fn."""
     if kind not in KINDS:
         raise TypeError(f"unsupported 8-bit type {kind}")
-    _rows("x", x)
-    q = _out("q", q, x, kind)
+    operand = _operand(x)
+    shape = operand[0]
+    q = torch.empty_like(x, dtype=kind, memory_format=torch.contiguous_format) if q is None else _out("q", q, shape, kind)
     if scale is None:
-        scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    _vector("scale", scale, x.shape[0])
-    return q, scale, _forward(_FWD_Q8, x, weight, eps, residual, h, q, None, scale, KINDS[kind])
+        scale = weight.new_empty(shape[0])
+    _vector("scale", scale, shape[0])
+    return q, scale, _forward(_FWD_Q8, x, weight, eps, residual, h, q, None, scale, KINDS[kind], operand)
 
 
 def mtfm_rms_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, dh: Optional[torch.Tensor] = None,
                  workspace: Optional[torch.Tensor] = None, out=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(dx, dweight) for the gradients dy of y and dh of h; dx is the gradient of x and of the residual.  `out` may hold preallocated
     (dx, dweight); dx may be dy or dh."""
-    code, h_stride = _dtype_code(h), _rows("h", h)
-    n, d = h.shape
-    dy_stride = _rows("dy", dy, h)
-    dh_stride = 0 if dh is None else _rows("dh", dh, h)
+    shape, dtype, code = _operand(h)
+    n, d = shape
+    h_stride, dy_stride = _rows("h", h, shape, dtype), _rows("dy", dy, shape, dtype)
+    dh_stride = 0 if dh is None else _rows("dh", dh, shape, dtype)
     _vector("weight", weight, d)
     _vector("rstd", rstd, n)
     dx, dweight = out or (None, None)
-    dx = _out("dx", dx, h)
+    dx = torch.empty_like(h, memory_format=torch.contiguous_format) if dx is None else _out("dx", dx, shape, dtype)
     if dweight is None:
         dweight = torch.empty_like(weight)
     _vector("dweight", dweight, d)
     if workspace is None:
         workspace = torch.empty(max(mtfm_rms_bwd_workspace_bytes(d), 256), dtype=torch.uint8, device=h.device)
-    if not workspace.is_contiguous():
+    elif not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     hta.check_on_current_device(dy, h, weight, rstd, dh, dx, dweight, workspace)
     P = hta._address
