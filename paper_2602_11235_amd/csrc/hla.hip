@@ -848,17 +848,14 @@ int check_sizes(int layer, int dtype, int32_t batch, int64_t total_q, int64_t to
     return MTFM_HTA_OK;
 }
 
-constexpr int ORDER_RATIO = 2;
 constexpr int MIN_SEG = 256;  // rows of a piece at least; a multiple of what a chunk has
-constexpr int PER_CU(int d) { return d == 128 ? 2 : 4; }  // workgroups that a compute unit holds
-
 // rows of a chunk
-constexpr int sweep_rows(int D) { return D == 128 ? 32 : 64; }
+constexpr int sweep_rows(int D, bool FULL) { return D == 128 && FULL ? 32 : 64; }
 constexpr int BACK_ROWS = 64, STATES_ROWS = 32;
 
 // heads of a group that a backward workgroup holds: what registers allow of the largest power of two that divides the group
-int heads_per_workgroup(int ratio, int d) {
-    const int most = d == 128 ? 2 : 4;
+int heads_per_workgroup(int ratio, int d, bool full) {
+    const int most = d == 128 && full ? 2 : 4;
     int g = 1;
     while (2 * g <= most && ratio % (2 * g) == 0) g *= 2;
     return g;
@@ -874,24 +871,26 @@ struct Plan {
 };
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-Plan plan_of(bool backward, int batch, int64_t total_kv, int max_hist, int max_targets, int Hq, int Hkv, int d) {
+Plan plan_of(bool backward, bool full, int batch, int64_t total_kv, int max_hist, int max_targets, int Hq, int Hkv, int d) {
     Plan p = {};
-    p.G = heads_per_workgroup(Hq / Hkv, d);
+    p.G = heads_per_workgroup(Hq / Hkv, d, full);
     p.spread = Hq / Hkv / p.G;
     p.partial = backward && p.spread > 1 ? align256((size_t)p.spread * total_kv * Hkv * d * sizeof(float)) : 0;
-    // Pieces: where users' heads do not fill the chip, a user's history is cut until they do.
-    const int places = 256 * PER_CU(d);
-    const int64_t whole = (int64_t)batch * Hq;
-    const int64_t cuts = places / whole - 1;  // (and a piece for the candidates)
-    if (cuts >= 2 && max_hist >= 2 * MIN_SEG) {
-        p.seg = ceil_div(ceil_div(max_hist, cuts), MOST_ROWS) * MOST_ROWS;
-        if (p.seg < MIN_SEG) p.seg = MIN_SEG;
-        p.n_hist = ceil_div(max_hist, p.seg), p.n_tgt = ceil_div(max_targets, p.seg);
+    // Pieces.  A user's head is one workgroup's work, so a call lasts as long as the longest history takes by itself, at least; cut into pieces, whose states take
+    // another reading of half a sweep's work and two launches, it lasts as long as the chip needs for all rows.  `mean`: rows of a place on a full chip;
+    // us of a row there, and of a row of a workgroup that is alone on its compute unit (backwards: with dk and dv).
+    const int places = 256 * (d == 128 ? 2 : 4);
+    const int64_t whole = (int64_t)batch * Hq, mean = total_kv * Hq / places;
+    const double full_row = d == 128 ? 0.117 : 0.094, lone_row = d == 128 ? 0.047 : 0.016, passes = backward ? 2 : 1;
+    const int64_t seg = mean <= MIN_SEG ? MIN_SEG : (mean + MOST_ROWS - 1) / MOST_ROWS * MOST_ROWS;
+    const double cost = 0.5 * passes * full_row * (double)mean + 15, gain = ((double)max_hist - (double)seg) * lone_row * (backward ? 1 + p.G : 1);
+    if (max_hist >= 2 * seg && cost < gain) {
+        p.seg = (int)seg, p.n_hist = ceil_div(max_hist, seg), p.n_tgt = ceil_div(max_targets, seg);
         p.states = align256((size_t)whole * (p.n_hist + p.n_tgt + 1) * d * d * sizeof(float));
     }
     // Long users first, where lengths differ and there are more of them than places: the last ones to start are short.  (A launch of 4 us.)
     const bool even = (double)total_kv >= 0.9 * (double)batch * ((double)max_hist + max_targets);
-    if (!p.seg && !even && whole * ORDER_RATIO > places && max_hist > MIN_SEG) p.order = align256(hta::schedule_bytes(batch));
+    if (!p.seg && !even && 2 * whole > places && max_hist > MIN_SEG) p.order = align256(hta::schedule_bytes(batch));
     return p;
 }
 
@@ -912,8 +911,8 @@ int64_t grid_of(const Args& a, int members) {
 template <int D>
 hipError_t launch_sweep_d(const Args& a, hipStream_t s) {
     const dim3 grid((unsigned)grid_of(a, a.ratio));
-    if (a.full) hipLaunchKernelGGL((sweep_kernel<D, sweep_rows(D), true>), grid, dim3(D * 4), 0, s, a);
-    else hipLaunchKernelGGL((sweep_kernel<D, sweep_rows(D), false>), grid, dim3(D * 4), 0, s, a);
+    if (a.full) hipLaunchKernelGGL((sweep_kernel<D, sweep_rows(D, true), true>), grid, dim3(D * 4), 0, s, a);
+    else hipLaunchKernelGGL((sweep_kernel<D, sweep_rows(D, false), false>), grid, dim3(D * 4), 0, s, a);
     return hipGetLastError();
 }
 hipError_t launch_sweep(const Args& a, int d, hipStream_t s) {
@@ -949,15 +948,15 @@ hipError_t launch_back_as(const Args& a, hipStream_t s) {
     hipLaunchKernelGGL((back_kernel<D, G, C, FULL>), dim3((unsigned)grid_of(a, a.spread)), dim3(D * 4), lds, s, a);
     return hipGetLastError();
 }
-template <int D, int G>
-hipError_t launch_back_layer(const Args& a, hipStream_t s) { return a.full ? launch_back_as<D, G, true>(a, s) : launch_back_as<D, G, false>(a, s); }
-template <int D>
-hipError_t launch_back_d(const Args& a, int G, hipStream_t s) {
-    if (G == 1) return launch_back_layer<D, 1>(a, s);
-    if (G == 2) return launch_back_layer<D, 2>(a, s);
-    if constexpr (D < 128) return launch_back_layer<D, 4>(a, s);
-    return hipErrorInvalidValue;
+template <int D, bool FULL>
+hipError_t launch_back_layer(const Args& a, int G, hipStream_t s) {
+    if (G == 1) return launch_back_as<D, 1, FULL>(a, s);
+    if constexpr (D < 128 || !FULL)
+        if (G == 4) return launch_back_as<D, 4, FULL>(a, s);
+    return launch_back_as<D, 2, FULL>(a, s);
 }
+template <int D>
+hipError_t launch_back_d(const Args& a, int G, hipStream_t s) { return a.full ? launch_back_layer<D, true>(a, G, s) : launch_back_layer<D, false>(a, G, s); }
 hipError_t launch_back(const Args& a, int d, int G, hipStream_t s) {
     return d == 32 ? launch_back_d<32>(a, G, s) : d == 64 ? launch_back_d<64>(a, G, s) : launch_back_d<128>(a, G, s);
 }
@@ -1014,7 +1013,7 @@ size_t mtfm_hla_workspace_bytes(int layer, int dtype, int is_bwd, int32_t batch,
                                 int32_t Hq, int32_t Hkv, int32_t head_dim) {
     if (hla::check_sizes(layer, dtype, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, head_dim) != MTFM_HTA_OK) return (size_t)-1;
     if (batch == 0) return 0;
-    const hla::Plan plan = hla::plan_of(is_bwd, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
+    const hla::Plan plan = hla::plan_of(is_bwd, layer == MTFM_HTA_LAYER_FULL, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
     return plan.bytes(is_bwd);
 }
 
@@ -1025,7 +1024,7 @@ int mtfm_hla_fwd(const void* q, const void* k, const void* v, const float* log_d
     if (int rc = hla::check_sizes(layer, dtype, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, head_dim)) return rc;
     if (batch == 0) return MTFM_HTA_OK;
     if (int rc = hla::check_arrays({q, out}, {k, v}, {state, final_state}, log_decay, {q_offsets, kv_offsets, hist_len, n_targets}, total_q, total_kv, scale)) return rc;
-    const hla::Plan plan = hla::plan_of(false, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
+    const hla::Plan plan = hla::plan_of(false, layer == MTFM_HTA_LAYER_FULL, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
     if (int rc = hla::check_workspace(plan.bytes(false), workspace, workspace_bytes)) return rc;
     hla::Args a = hla::args_of(log_decay, q_offsets, kv_offsets, hist_len, n_targets, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, scale, layer);
     a.seg = plan.seg, a.n_hist = plan.n_hist, a.n_tgt = plan.n_tgt, a.states = (float*)((char*)workspace + plan.order);
@@ -1051,7 +1050,7 @@ int mtfm_hla_bwd(const void* dout, const void* q, const void* k, const void* v, 
     if (int rc = hla::check_arrays({dout, q, dq}, {k, v, dk, dv}, {state, dfinal_state, dstate}, log_decay, {q_offsets, kv_offsets, hist_len, n_targets}, total_q,
                                    total_kv, scale))
         return rc;
-    const hla::Plan plan = hla::plan_of(true, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
+    const hla::Plan plan = hla::plan_of(true, layer == MTFM_HTA_LAYER_FULL, batch, total_kv, max_hist, max_targets, Hq, Hkv, head_dim);
     if (int rc = hla::check_workspace(plan.bytes(true), workspace, workspace_bytes)) return rc;
     hla::Args a = hla::args_of(log_decay, q_offsets, kv_offsets, hist_len, n_targets, batch, total_q, total_kv, max_hist, max_targets, Hq, Hkv, scale, layer);
     hipStream_t s = (hipStream_t)stream;
