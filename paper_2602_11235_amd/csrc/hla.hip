@@ -877,15 +877,22 @@ Plan plan_of(bool backward, bool full, int batch, int64_t total_kv, int max_hist
     p.spread = Hq / Hkv / p.G;
     p.partial = backward && p.spread > 1 ? align256((size_t)p.spread * total_kv * Hkv * d * sizeof(float)) : 0;
     // Pieces.  A user's head is one workgroup's work, so a call lasts as long as the longest history takes by itself, at least; cut into pieces, whose states take
-    // another reading of half a sweep's work and two launches, it lasts as long as the chip needs for all rows.  `mean`: rows of a place on a full chip;
-    // us of a row there, and of a row of a workgroup that is alone on its compute unit (backwards: with dk and dv).
+    // another reading of half a sweep's work and two launches, it lasts as long as the chip needs for all rows, and a third more (pieces do not fill the places
+    // evenly).  `mean`: rows of a place on a full chip; the others: us of a row there, and of a row of a workgroup that is alone on its compute unit, in a
+    // sweep and in the sweep for dk and dv (of a head), as measured.
     const int places = 256 * (d == 128 ? 2 : 4);
-    const int64_t whole = (int64_t)batch * Hq, mean = total_kv * Hq / places;
-    const double full_row = d == 128 ? 0.117 : 0.094, lone_row = d == 128 ? 0.047 : 0.016, passes = backward ? 2 : 1;
-    const int64_t seg = mean <= MIN_SEG ? MIN_SEG : (mean + MOST_ROWS - 1) / MOST_ROWS * MOST_ROWS;
-    const double cost = 0.5 * passes * full_row * (double)mean + 15, gain = ((double)max_hist - (double)seg) * lone_row * (backward ? 1 + p.G : 1);
-    if (max_hist >= 2 * seg && cost < gain) {
-        p.seg = (int)seg, p.n_hist = ceil_div(max_hist, seg), p.n_tgt = ceil_div(max_targets, seg);
+    const int64_t whole = (int64_t)batch * Hq;
+    const double mean = (double)total_kv * Hq / places, longest = max_hist;
+    const double full_row = full ? (d == 128 ? 0.117 : 0.094) : (d == 128 ? 0.052 : 0.035), lone_row = full ? (d == 128 ? 0.06 : 0.036) : (d == 128 ? 0.035 : 0.016);
+    const double full_back = d == 128 ? 0.22 : 0.13, lone_back = d == 128 ? 0.08 : 0.05;
+    const int seg = mean <= 2 * MIN_SEG ? MIN_SEG : ceil_div((int64_t)(mean / 2), MOST_ROWS) * MOST_ROWS;
+    double one = std::max(mean * full_row, longest * lone_row), cut = std::max(1.3 * mean * full_row, seg * lone_row) * (full ? 1.5 : 1.0) + 15;
+    if (backward) {
+        one += std::max(mean * full_back, longest * p.G * lone_back);
+        cut += std::max(1.3 * mean * full_back, seg * p.G * lone_back) + 0.5 * std::max(1.3 * mean * full_row, seg * lone_row) + 5;
+    }
+    if (max_hist >= 2 * seg && cut < one) {
+        p.seg = seg, p.n_hist = ceil_div(max_hist, seg), p.n_tgt = ceil_div(max_targets, seg);
         p.states = align256((size_t)whole * (p.n_hist + p.n_tgt + 1) * d * d * sizeof(float));
     }
     // Long users first, where lengths differ and there are more of them than places: the last ones to start are short.  (A launch of 4 us.)
