@@ -942,11 +942,18 @@ hipError_t launch_states(const Args& a, int d, int first_job, int jobs, const fl
     return e;
 }
 
-// Lets a kernel use its dynamic LDS; asked for once per kernel, not a stream operation (a graph that is being captured does not see it).
+// Lets a kernel use its dynamic LDS; asked for once per kernel and device, not a stream operation (a graph that is being captured does not see it).
 template <auto Kernel>
 hipError_t allow_lds(int bytes) {
-    static hipError_t state = hipFuncSetAttribute((const void*)Kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    return state;
+    constexpr int MAX_DEVICES = 64;
+    static std::atomic<bool> allowed[MAX_DEVICES];
+    int dev = 0;
+    if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+    const bool known = dev >= 0 && dev < MAX_DEVICES;
+    if (known && allowed[dev].load(std::memory_order_relaxed)) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute((const void*)Kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (known && e == hipSuccess) allowed[dev].store(true, std::memory_order_relaxed);
+    return e;
 }
 template <int D, int G, bool FULL>
 hipError_t launch_back_as(const Args& a, hipStream_t s) {

@@ -343,8 +343,9 @@ hipError_t launch_as(Args& a, float* dweight, int* shares, hipStream_t s) {
         return hipGetLastError();
     }
     constexpr int NTHR = bwd_threads(TPR);
-    *shares = grid_for(a.n, NTHR / TPR, MAX_SHARES);
-    if (*shares == 1) a.partials = dweight;  // a single workgroup's share is the sum
+    // up to four turns of one workgroup: its share is the sum, and a second launch costs as much
+    *shares = a.n <= 4 * (NTHR / TPR) ? 1 : grid_for(a.n, NTHR / TPR, MAX_SHARES);
+    if (*shares == 1) a.partials = dweight;
     hipLaunchKernelGGL((bwd_kernel<T, V, TPR, NG>), dim3(*shares), dim3(NTHR), 0, s, a);
     return hipGetLastError();
 }

@@ -50,6 +50,7 @@ def _call(fields) -> None:
         raise hta.HtaError(status, hta.mtfm_hta_last_error())
 
 
+_workspace_words = {}  # of a backward call, by width (host arithmetic that never changes)
 _CODES = {torch.bfloat16: hta.BF16, torch.float32: hta.FP32}
 
 
@@ -153,7 +154,10 @@ def mtfm_rms_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: 
         dweight = torch.empty_like(weight)
     _vector("dweight", dweight, d)
     if workspace is None:
-        workspace = torch.empty(max(mtfm_rms_bwd_workspace_bytes(d), 256), dtype=torch.uint8, device=h.device)
+        words = _workspace_words.get(d)
+        if words is None:
+            words = _workspace_words[d] = max(mtfm_rms_bwd_workspace_bytes(d), 256) // 4
+        workspace = weight.new_empty(words)
     elif not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     hta.check_on_current_device(dy, h, weight, rstd, dh, dx, dweight, workspace)
