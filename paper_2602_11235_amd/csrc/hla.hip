@@ -853,13 +853,8 @@ constexpr int MIN_SEG = 256;  // rows of a piece at least; a multiple of what a 
 constexpr int sweep_rows(int D, bool FULL) { return D == 128 && FULL ? 32 : 64; }
 constexpr int BACK_ROWS = 64, STATES_ROWS = 32;
 
-// heads of a group that a backward workgroup holds: what registers allow of the largest power of two that divides the group
-int heads_per_workgroup(int ratio, int d, bool full) {
-    const int most = d == 128 && full ? 2 : 4;
-    int g = 1;
-    while (2 * g <= most && ratio % (2 * g) == 0) g *= 2;
-    return g;
-}
+// heads of a group that a backward workgroup may hold: what registers allow
+int most_heads(int d, bool full) { return d == 128 && full ? 2 : 4; }
 
 struct Plan {
     int G, spread;      // backwards: heads of a group to a workgroup, workgroups to a group
@@ -873,26 +868,39 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 Plan plan_of(bool backward, bool full, int batch, int64_t total_kv, int max_hist, int max_targets, int Hq, int Hkv, int d) {
     Plan p = {};
-    p.G = heads_per_workgroup(Hq / Hkv, d, full);
-    p.spread = Hq / Hkv / p.G;
-    p.partial = backward && p.spread > 1 ? align256((size_t)p.spread * total_kv * Hkv * d * sizeof(float)) : 0;
-    // Pieces.  A user's head is one workgroup's work, so a call lasts as long as the longest history takes by itself, at least; cut into pieces, whose states take
-    // another reading of half a sweep's work and two launches, it lasts as long as the chip needs for all rows, and a third more (pieces do not fill the places
-    // evenly).  `mean`: rows of a place on a full chip; the others: us of a row there, and of a row of a workgroup that is alone on its compute unit, in a
-    // sweep and in the sweep for dk and dv (of a head), as measured.
-    const int places = 256 * (d == 128 ? 2 : 4);
+    // How a call is cut up goes by the time of each way, in us.  A user's head is one workgroup's work, so a sweep lasts as long as the longest history takes by
+    // itself, at least; cut into pieces, whose states take another reading of half a sweep's work and two launches, it lasts as long as the chip needs for all
+    // rows, and a third more (pieces do not fill the places evenly).  The heads of a group that a backward workgroup does not hold are summed by a launch of its
+    // own, over shares that are written and read.  `mean`: rows of a place on a full chip; us of a row there, and of a row of a workgroup that is alone on
+    // its compute unit, in a sweep and (of a head) in the sweep for dk and dv: as measured.
+    const int places = 256 * (d == 128 ? 2 : 4), ratio = Hq / Hkv;
     const int64_t whole = (int64_t)batch * Hq;
-    const double mean = (double)total_kv * Hq / places, longest = max_hist;
+    const double mean = (double)total_kv * Hq / places;
     const double full_row = full ? (d == 128 ? 0.117 : 0.094) : (d == 128 ? 0.052 : 0.035), lone_row = full ? (d == 128 ? 0.06 : 0.036) : (d == 128 ? 0.035 : 0.016);
-    const double full_back = d == 128 ? 0.22 : 0.13, lone_back = d == 128 ? 0.08 : 0.05;
+    const double full_back = d == 128 ? 0.22 : 0.13, lone_back = full ? (d == 128 ? 0.08 : 0.05) : (d == 128 ? 0.05 : 0.03), start = 6;
     const int seg = mean <= 2 * MIN_SEG ? MIN_SEG : ceil_div((int64_t)(mean / 2), MOST_ROWS) * MOST_ROWS;
-    double one = std::max(mean * full_row, longest * lone_row), cut = std::max(1.3 * mean * full_row, seg * lone_row) * (full ? 1.5 : 1.0) + 15;
-    if (backward) {
-        one += std::max(mean * full_back, longest * p.G * lone_back);
-        cut += std::max(1.3 * mean * full_back, seg * p.G * lone_back) + 0.5 * std::max(1.3 * mean * full_row, seg * lone_row) + 5;
+    const auto sweep = [&](double fill, double rows) { return std::max(fill * mean * full_row, rows * lone_row) + start; };
+    double best = 0;
+    for (int G = most_heads(d, full); G >= 1; G /= 2) {
+        if (ratio % G != 0 || (!backward && G > 1)) continue;
+        for (int cut = 0; cut <= (max_hist >= 2 * seg); cut++) {
+            const double fill = cut ? 1.3 : 1.0, rows = cut ? seg : max_hist;
+            // (a history that does not ask is nothing but its states; they are written, summed and read)
+            const double states = cut ? (full ? 0.5 : 1.0) * sweep(fill, rows) + start + (double)whole * (ceil_div(max_hist, seg) + 2) * d * d * 8 / 4.9e6 : 0;
+            double time = (full || !cut ? sweep(fill, rows + max_targets) : start) + states;
+            if (backward) {
+                time += std::max(fill * mean * full_back, (rows + max_targets) * G * lone_back) + start + (full ? states : 0);
+                if (ratio > G) time += start + (double)total_kv * Hq / G * d * 16 / 4.9e6;
+            }
+            if (best != 0 && time >= best) continue;
+            best = time;
+            p.G = G, p.seg = cut ? seg : 0;
+        }
     }
-    if (max_hist >= 2 * seg && cut < one) {
-        p.seg = seg, p.n_hist = ceil_div(max_hist, seg), p.n_tgt = ceil_div(max_targets, seg);
+    p.spread = ratio / p.G;
+    p.partial = backward && p.spread > 1 ? align256((size_t)p.spread * total_kv * Hkv * d * sizeof(float)) : 0;
+    if (p.seg) {
+        p.n_hist = ceil_div(max_hist, seg), p.n_tgt = ceil_div(max_targets, seg);
         p.states = align256((size_t)whole * (p.n_hist + p.n_tgt + 1) * d * d * sizeof(float));
     }
     // Long users first, where lengths differ and there are more of them than places: the last ones to start are short.  (A launch of 4 us.)
