@@ -839,12 +839,16 @@ int check_heads(int32_t Hq, int32_t Hkv, int32_t d, int dtype) {
     return MTFM_HTA_OK;
 }
 
+constexpr int64_t MOST_TOKENS = (int64_t)1 << 30;  // (the last piece or chunk may end behind them, in 32 bits)
+// A launch has less than 2^32 threads: 4 head_dim to a workgroup, or 256 of the scan; 8 groups of heads may be none.
+bool launchable(int64_t workgroups, int d) { return workgroups * std::max(4 * d, 256) < ((int64_t)1 << 32) - ((int64_t)1 << 26); }
+
 int check_sizes(int layer, int dtype, int32_t batch, int64_t total_q, int64_t total_kv, int32_t max_hist, int32_t max_targets, int32_t Hq, int32_t Hkv, int32_t d) {
     if (int rc = check_heads(Hq, Hkv, d, dtype)) return rc;
     if (layer != MTFM_HTA_LAYER_FULL && layer != MTFM_HTA_LAYER_TARGET) return hta::report_error(MTFM_HTA_ERR_INVALID_ARG, "unknown layer kind %d", layer);
     if (batch < 0 || total_q < 0 || total_kv < 0 || max_hist < 0 || max_targets < 0) return hta::report_error(MTFM_HTA_ERR_INVALID_ARG, "negative size");
-    if (total_q > INT32_MAX || total_kv > INT32_MAX) return hta::report_error(MTFM_HTA_ERR_UNSUPPORTED, "more than 2^31 - 1 rows");
-    if ((int64_t)batch * Hq > (int64_t)1 << 26) return hta::report_error(MTFM_HTA_ERR_UNSUPPORTED, "batch (%d) x Hq (%d) exceeds 2^26", batch, Hq);
+    if (total_q > MOST_TOKENS || total_kv > MOST_TOKENS) return hta::report_error(MTFM_HTA_ERR_UNSUPPORTED, "more than 2^30 rows");
+    if (!launchable((int64_t)batch * Hq, d)) return hta::report_error(MTFM_HTA_ERR_UNSUPPORTED, "batch (%d) x Hq (%d) x head_dim (%d) are too many for a launch", batch, Hq, d);
     return MTFM_HTA_OK;
 }
 
@@ -868,6 +872,7 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 Plan plan_of(bool backward, bool full, int batch, int64_t total_kv, int max_hist, int max_targets, int Hq, int Hkv, int d) {
     Plan p = {};
+    max_hist = (int)std::min((int64_t)max_hist, total_kv), max_targets = (int)std::min((int64_t)max_targets, total_kv);
     // How a call is cut up goes by the time of each way, in us.  A user's head is one workgroup's work, so a sweep lasts as long as the longest history takes by
     // itself, at least; cut into pieces, whose states take another reading of half a sweep's work and two launches, it lasts as long as the chip needs for all
     // rows, and a third more (pieces do not fill the places evenly).  The heads of a group that a backward workgroup does not hold are summed by a launch of its
@@ -878,12 +883,13 @@ Plan plan_of(bool backward, bool full, int batch, int64_t total_kv, int max_hist
     const double mean = (double)total_kv * Hq / places;
     const double full_row = full ? (d == 128 ? 0.117 : 0.094) : (d == 128 ? 0.052 : 0.035), lone_row = full ? (d == 128 ? 0.06 : 0.036) : (d == 128 ? 0.035 : 0.016);
     const double full_back = d == 128 ? 0.22 : 0.13, lone_back = full ? (d == 128 ? 0.08 : 0.05) : (d == 128 ? 0.05 : 0.03), start = 6;
-    const int seg = mean <= 2 * MIN_SEG ? MIN_SEG : ceil_div((int64_t)(mean / 2), MOST_ROWS) * MOST_ROWS;
+    const int seg = mean <= 2 * MIN_SEG ? MIN_SEG : ceil_div((int64_t)std::min(mean / 2, MOST_TOKENS / 2.), MOST_ROWS) * MOST_ROWS;
     const auto sweep = [&](double fill, double rows) { return std::max(fill * mean * full_row, rows * lone_row) + start; };
+    const int pieces = ceil_div(max_hist, seg) + ceil_div(max_targets, seg);
     double best = 0;
     for (int G = most_heads(d, full); G >= 1; G /= 2) {
         if (ratio % G != 0 || (!backward && G > 1)) continue;
-        for (int cut = 0; cut <= (max_hist >= 2 * seg); cut++) {
+        for (int cut = 0; cut <= (max_hist >= 2 * seg && launchable(whole * pieces, d)); cut++) {
             const double fill = cut ? 1.3 : 1.0, rows = cut ? seg : max_hist;
             // (a history that does not ask is nothing but its states; they are written, summed and read)
             const double states = cut ? (full ? 0.5 : 1.0) * sweep(fill, rows) + start + (double)whole * (ceil_div(max_hist, seg) + 2) * d * d * 8 / 4.9e6 : 0;
@@ -1107,7 +1113,7 @@ int mtfm_hla_step(const void* q, const void* k, const void* v, const float* log_
                   int32_t n_rows, int32_t n_slots, int32_t Hq, int32_t Hkv, int32_t head_dim, float scale, int dtype, void* stream) {
     if (int rc = hla::check_heads(Hq, Hkv, head_dim, dtype)) return rc;
     if (n_rows < 0 || n_slots < 0) return hta::report_error(MTFM_HTA_ERR_INVALID_ARG, "negative size");
-    if ((int64_t)n_rows * Hq > (int64_t)1 << 26) return hta::report_error(MTFM_HTA_ERR_UNSUPPORTED, "n_rows (%d) x Hq (%d) exceeds 2^26", n_rows, Hq);
+    if (!hla::launchable((int64_t)n_rows * Hq, 32)) return hta::report_error(MTFM_HTA_ERR_UNSUPPORTED, "n_rows (%d) x Hq (%d) are too many for a launch", n_rows, Hq);
     if (n_rows == 0) return MTFM_HTA_OK;
     if (!(scale > 0.f) || !(scale < INFINITY)) return hta::report_error(MTFM_HTA_ERR_INVALID_ARG, "scale must be positive and finite");
     if (!q || !k || !v || !log_decay || !out || (n_slots > 0 && (!state || !new_state))) return hta::report_error(MTFM_HTA_ERR_INVALID_ARG, "null pointer argument");

@@ -115,3 +115,24 @@ def test_binding_refuses_steps_that_do_not_fit():
             make(**kw)
     with pytest.raises(ValueError, match="current GPU"):
         make()
+
+
+@pytest.mark.parametrize("back", (False, True))
+@pytest.mark.parametrize("kw", [dict(batch=1 << 24, Hq=1, Hkv=1), dict(batch=1 << 20, Hq=16, Hkv=1), dict(batch=1 << 20, Hq=8, Hkv=8, d=128),
+                                dict(total_kv=(1 << 30) + 1), dict(total_q=(1 << 30) + 1)])
+def test_more_than_a_launch_takes_is_refused(kw, back):
+    assert call(back, **kw) == hta.ERR_UNSUPPORTED
+
+
+def test_more_steps_than_a_launch_takes_are_refused():
+    assert step(rows=1 << 21, n_slots=1 << 21) == hta.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("total", (10, 5000, 1 << 30))
+@pytest.mark.parametrize("heads", ((4, 2, 64), (16, 1, 128), (1, 1, 32)))
+def test_bounds_beyond_the_rows_ask_for_no_more_workspace(total, heads):
+    for back in (False, True):
+        need = [hla.mtfm_hla_workspace_bytes(layer, hta.BF16, back, 2, total, total, most, most, *heads)
+                for layer in (hta.LAYER_FULL, hta.LAYER_TARGET) for most in (total, (1 << 31) - 1)]
+        assert need[0] == need[1] and need[2] == need[3]
+        assert max(need) <= 40 * total * heads[0] * heads[2] + (1 << 20)  # (shares of 8 bytes to an element, and states of pieces of a few hundred rows)
