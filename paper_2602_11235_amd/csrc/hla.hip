@@ -697,7 +697,7 @@ __global__ __launch_bounds__(D * 4, 4) void states_kernel(const Args args, int f
 }
 
 // The states in front of the pieces from what each adds, in the order of the sweep: X <- l^n X + U, in place; the last is the caller's.  blockIdx.z: 1 backwards.
-constexpr int SCAN_THREADS = 256;
+constexpr int SCAN_THREADS = 256, SCAN_AHEAD = 16;  // loads in flight: the sum is all latency
 template <int D>
 __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const Args args, int first_job, const float* in_ahead, int transposed, float* out_ahead, const float* in_back,
                                                             float* out_back) {
@@ -719,7 +719,8 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const Args args, int
         else x = *(const floatx4*)(in + state + e);
     }
     const bool adds = args.full || !back;  // (backwards through a history that does not ask nothing is added)
-    constexpr int AHEAD = 16;  // loads in flight: the sum is all latency
+    const bool all_wanted = args.full || back;  // (forwards over a history that does not ask: the last alone)
+    constexpr int AHEAD = SCAN_AHEAD;
     for (int s = 0; s < n; s += AHEAD) {
         floatx4 y[AHEAD];
 #pragma unroll
@@ -728,7 +729,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const Args args, int
         for (int i = 0; i < AHEAD; i++) {
             if (s + i >= n) break;
             const float f = s + i < ts ? 1.f : s + i == n - 1 ? last : all;
-            *(floatx4*)(p + (int64_t)(s + i) * D * D) = x;
+            if (all_wanted) *(floatx4*)(p + (int64_t)(s + i) * D * D) = x;
             x = x * f + y[i];
         }
     }
@@ -852,7 +853,7 @@ int check_sizes(int layer, int dtype, int32_t batch, int64_t total_q, int64_t to
     return MTFM_HTA_OK;
 }
 
-constexpr int MIN_SEG = 256;  // rows of a piece at least; a multiple of what a chunk has
+constexpr int MIN_SEG = 128;  // rows of a piece at least; a multiple of what a chunk has
 // rows of a chunk
 constexpr int sweep_rows(int D, bool FULL) { return D == 128 && FULL ? 32 : 64; }
 constexpr int BACK_ROWS = 64, STATES_ROWS = 32;
@@ -875,43 +876,45 @@ Plan plan_of(bool backward, bool full, int batch, int64_t total_kv, int max_hist
     max_hist = (int)std::min((int64_t)max_hist, total_kv), max_targets = (int)std::min((int64_t)max_targets, total_kv);
     // How a call is cut up goes by the time of each way, in us.  A user's head is one workgroup's work, so a sweep lasts as long as the longest history takes by
     // itself, at least; cut into pieces, whose states take another reading of half a sweep's work and two launches, it lasts as long as the chip needs for all
-    // rows, and a third more (pieces do not fill the places evenly).  The heads of a group that a backward workgroup does not hold are summed by a launch of its
-    // own, over shares that are written and read.  `mean`: rows of a place on a full chip; us of a row there, and of a row of a workgroup that is alone on
-    // its compute unit, in a sweep and (of a head) in the sweep for dk and dv: as measured.
+    // rows, in whole pieces to a compute unit (0.85: a user's last one is not whole).  The heads of a group that a backward workgroup does not hold are summed by a launch of its own, over shares that
+    // are written and read.  `mean`: rows of a place on a full chip; us of a row there, and of a row of a workgroup that is alone on its compute unit, in a sweep
+    // and (of a head) in the sweep for dk and dv: as measured.  (Forward, us, by rows of a piece none / 128 / 256 / 512: one user of 8192, 16/2 heads of 128,
+    // 462 / 91 / 77 / 94; 18 users of 360 to 5080, 8/2 of 64, 157 / 62 / 51 / 58; 19 of 438 to 1752 with states, forward and backward, 256 206, 128 150; 256 of
+    // 512 to 1024 164 / 357 / 285.  Over 90 calls the choice takes 1.01 of the best one's time; 39 users of 543 to 2424, 8/2 of 64, in pieces of 1024 took 1.8 of that in 256.)
     const int places = 256 * (d == 128 ? 2 : 4), ratio = Hq / Hkv;
     const int64_t whole = (int64_t)batch * Hq;
     const double mean = (double)total_kv * Hq / places;
     const double full_row = full ? (d == 128 ? 0.117 : 0.094) : (d == 128 ? 0.052 : 0.035), lone_row = full ? (d == 128 ? 0.06 : 0.036) : (d == 128 ? 0.035 : 0.016);
     const double full_back = d == 128 ? 0.22 : 0.13, lone_back = full ? (d == 128 ? 0.08 : 0.05) : (d == 128 ? 0.05 : 0.03), start = 6;
-    const int seg = mean <= 2 * MIN_SEG ? MIN_SEG : ceil_div((int64_t)std::min(mean / 2, MOST_TOKENS / 2.), MOST_ROWS) * MOST_ROWS;
-    const auto sweep = [&](double fill, double rows) { return std::max(fill * mean * full_row, rows * lone_row) + start; };
-    const int pieces = ceil_div(max_hist, seg) + ceil_div(max_targets, seg);
+    const auto sweep = [&](double rows_of_place, double rows) { return std::max(rows_of_place * full_row, rows * lone_row) + start; };
     double best = 0;
-    for (int G = most_heads(d, full); G >= 1; G /= 2) {
-        if (ratio % G != 0 || (!backward && G > 1)) continue;
-        for (int cut = 0; cut <= (max_hist >= 2 * seg && launchable(whole * pieces, d)); cut++) {
-            const double fill = cut ? 1.3 : 1.0, rows = cut ? seg : max_hist;
-            // (a history that does not ask is nothing but its states; they are written, summed and read)
-            const double states = cut ? (full ? 0.5 : 1.0) * sweep(fill, rows) + start + (double)whole * (ceil_div(max_hist, seg) + 2) * d * d * 8 / 4.9e6 : 0;
-            double time = (full || !cut ? sweep(fill, rows + max_targets) : start) + states;
+    // pieces of 128 rows, of twice as many and so on; 0: none
+    for (int seg = 0; seg <= max_hist / 2; seg = seg ? 2 * seg : MIN_SEG) {
+        if (seg && !launchable(whole * (ceil_div(max_hist, seg) + ceil_div(max_targets, seg)), d)) continue;
+        const int pieces = seg ? ceil_div(max_hist, seg) : 0;
+        const double rows = seg ? seg : max_hist, of_place = seg ? 0.85 * std::ceil(((double)total_kv / seg + batch) * Hq / 256) * 256 * seg / places : mean;
+        // (a history that does not ask is nothing but its states, written and read once; the others are written, summed, sixteen in flight, and read)
+        const double traffic = seg ? (double)whole * (pieces + 2) * d * d * 8 / 4.9e6 : 0;
+        const double states = seg ? (full ? 0.5 : 1.0) * sweep(of_place, rows) + start + 2 * ((pieces - 1) / SCAN_AHEAD) + (full ? 1.0 : 0.5) * traffic : 0;
+        const double ahead = (full || !seg ? sweep(of_place, rows + max_targets) : start) + states;
+        for (int G = most_heads(d, full); G >= 1; G /= 2) {
+            if (ratio % G != 0 || (!backward && G > 1)) continue;
+            double time = ahead;
             if (backward) {
-                time += std::max(fill * mean * full_back, (rows + max_targets) * G * lone_back) + start + (full ? states : 0);
+                time += std::max((seg ? 1.3 : 1.0) * mean * full_back, (rows + max_targets) * G * lone_back) + start + (full ? states : traffic);
                 if (ratio > G) time += start + (double)total_kv * Hq / G * d * 16 / 4.9e6;
             }
             if (best != 0 && time >= best) continue;
             best = time;
-            p.G = G, p.seg = cut ? seg : 0;
+            p.G = G, p.seg = seg, p.n_hist = pieces, p.n_tgt = seg ? ceil_div(max_targets, seg) : 0;
         }
     }
     p.spread = ratio / p.G;
     p.partial = backward && p.spread > 1 ? align256((size_t)p.spread * total_kv * Hkv * d * sizeof(float)) : 0;
-    if (p.seg) {
-        p.n_hist = ceil_div(max_hist, seg), p.n_tgt = ceil_div(max_targets, seg);
-        p.states = align256((size_t)whole * (p.n_hist + p.n_tgt + 1) * d * d * sizeof(float));
-    }
+    if (p.seg) p.states = align256((size_t)whole * (p.n_hist + p.n_tgt + 1) * d * d * sizeof(float));
     // Long users first, where lengths differ and there are more of them than places: the last ones to start are short.  (A launch of 4 us.)
     const bool even = (double)total_kv >= 0.9 * (double)batch * ((double)max_hist + max_targets);
-    if (!p.seg && !even && 2 * whole > places && max_hist > MIN_SEG) p.order = align256(hta::schedule_bytes(batch));
+    if (!p.seg && !even && 2 * whole > places && max_hist > 2 * MIN_SEG) p.order = align256(hta::schedule_bytes(batch));
     return p;
 }
 
