@@ -24,7 +24,7 @@
  * to 16 bits of significand, and no further than to 24 where the caller gets the state.  Rows that belong to no user (behind the last one's, or beyond hist_len + n_targets) are not
  * touched.  What a row may not see does not reach it, whatever it holds; what sees an infinity or a NaN is not finite (and may be
  * NaN where the formula gives an infinity).  max_hist and max_targets bound what is looked at: a longer history or list is cut there.
- * Hq * head_dim at most 2^22, total_q and total_kv at most 2^30, batch * Hq * max(4 head_dim, 256) less than 2^32 - 2^26.
+ * Hq * head_dim at most 2^22, total_q and total_kv at most 2^30, batch * Hq * max(4 head_dim, 256) less than 2^32 - 2^27.
  *
  * Pointers are DEVICE pointers owned by the caller; `stream` is a hipStream_t passed as void* (NULL = the default stream).  The
  * calls validate their scalar arguments on the host, enqueue kernels and return; they never allocate, copy to the host or
@@ -73,7 +73,7 @@ MTFM_HTA_API int mtfm_hla_bwd(const void* dout, const void* q, const void* k, co
  * (i itself if slots is NULL) of `state` and puts what follows into that slot of `new_state`, which may be `state` itself (else
  * they do not overlap); slots that no row names are not touched.  Rows that name the same slot are tokens of one user, in the
  * order of the rows.  A row whose slot is outside [0, n_slots) is padding: its output is zero.  `out` overlaps no input; n_rows * Hq
- * is less than 2^24 - 2^18.
+ * is less than 2^24 - 2^19.
  */
 MTFM_HTA_API int mtfm_hla_step(const void* q, const void* k, const void* v, const float* log_decay, const float* state,
                  float* new_state, const int32_t* slots, void* out, int32_t n_rows, int32_t n_slots, int32_t Hq, int32_t Hkv,

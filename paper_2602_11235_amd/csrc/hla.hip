@@ -3,15 +3,20 @@
 // All passes over a user's tokens are one sweep.  With rows a_i that ask, and pairs (b_i, c_i) that enter a state,
 //   S <- l S + b_i c_i^T,   o_i = scale a_i S
 // is the forward pass for (a, b, c) = (q, k, v); the gradients are the same sweep with the letters exchanged: dq for (dout, v, k)
-// in the same direction with the states transposed, and from the last row backwards dv for (k, q, dout) and dk for (v, dout, q).
+// in the same direction with the states transposed, and from the last row backwards dv for (k, q, dout) and dk for (v, dout, q), which
+// share the state (one has it transposed) and are one kernel.
 //
-// A workgroup owns a user's head and goes through the tokens in chunks of 64.  Inside a chunk, with i, j counted from its start and
+// A workgroup owns a user's head and goes through the tokens in chunks of 64 (or 32).  Inside a chunk, with i, j counted from its start and
 // S the state in front of it,
 //   o_i = scale [ l^(i+1) a_i S + sum_(j<=i) l^(i-j) <a_i, b_j> c_j ],    S <- l^n S + sum_j l^(n-1-j) b_j c_j^T:
-// four matrix products.  The work is bound by HBM (4 d^2 + 64 d operations per row and head on 8 d bytes), so a row is read once: the
+// four matrix products.  The floor is HBM's (4 d^2 + 64 d operations per row and head on 8 d bytes), so a row is read once: the
 // state stays in registers from chunk to chunk -- wave w owns its columns [16 w, 16 w + 16), whose accumulators are, rounded, the
 // operand of the product with a -- and the next chunk's rows are in flight while the current one is worked on.  Backwards the state is
 // handed on decayed already (o_i takes l^i, the update l^(n-j)), so that the gradient of S_L enters, and that of S_0 leaves, as it is.
+//
+// Roundings: operands of a product are bf16 (the state where rows ask it, weights between two products, results), sums float32.  What enters a state keeps 16
+// bits, in two parts of bf16, or 24, in three, where the state is what the caller gets: rounded to 8 it would be off by 2^-9 after the first token.
+// Long histories of few users are cut into pieces (plan_of): what each adds to a state, the states in front of them, then all of them at once.
 #include "../../include/mtfm_hla.h"
 #include "hta_common.h"
 #include "hta_mfma.h"
@@ -84,6 +89,7 @@ __device__ inline Piece piece_of(const Args& g, int id, int L, int T, bool back)
 // Tiles in LDS lie in rows of D elements without padding; the 16-byte word w of row r is at position w ^ place<D>(r).  A 16-byte read is served in groups of
 // 16 lanes, 0 .. 3, 12 .. 15 and 20 .. 27 the first (the bank conflicts of two lanes say so), an 8-byte read in groups of 32: with this order neither has a
 // conflict where 16 lanes read a word of 16 rows and the next 16 its neighbour, or a transposing read takes two words of 4 rows and of 4 rows 8 further.
+// (Forward, 212 548 rows, 8/2 heads of 64: 4.4 M cycles of conflicts of 31.6 M that LDS works, 14.3 M in the order before it, made for groups of neighbours.)
 template <int D>
 __device__ inline int place(int row) {
     const int h = (row >> 2) & 3, c = (((h ^ (h >> 1)) & 1) << 1) | (h >> 1);
@@ -324,6 +330,11 @@ struct Rows {  // of a chunk: n rows, row r is first + r (backwards through a hi
 
 // One sweep over a user's head in the tokens' order by a workgroup of D / 16 waves, each with 16 of the state's columns.  D[m][n] += A[m][k] B[k][n] of
 // 16x16x32: a lane holds row (column) lane % 16 and k = 8 (lane / 16) .. + 7 of either operand, and column lane % 16, rows 4 (lane / 16) .. + 3 of the result.
+//
+// 212 548 rows of 256 users, 8/2 heads of 64: 152 us = 3.6 TB/s of q, k, v and out (the first form 335; 196 with tables of the powers and 32-bit offsets, 160 with
+// one look for what is not finite, behind the product).  364 182 rows, 16/2 of 128: 1015 to 1032 us = 3.3 TB/s (1860, 1540, 1400 on that way; in chunks of 64
+// rows 4 % more).  No unit is full: at d = 64 the vector units are busy for 0.46 of the time, LDS for 0.42, the matrix units for 0.19, HBM for 0.7 of what a
+// copy reaches; the barriers of a chunk keep them from lying over each other.
 template <int D, int C, bool FULL>
 __global__ __launch_bounds__(D * 4, 4) void sweep_kernel(const Args args) {
     constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = C / PART, TILE = C * D * 2, IT = C / 16, KT = C / 32, TILES = IT * (IT + 1) / 2;
@@ -451,6 +462,10 @@ __global__ __launch_bounds__(D * 4, 4) void sweep_kernel(const Args args) {
 //   dv_i = l^i k_i R + scale sum_(j<=i) l^(i-j) <k_i, q_j> dout_j,     dk_i = l^i v_i R^T + scale sum_(j<=i) l^(i-j) <v_i, dout_j> q_j,
 //   R <- l^n R + scale sum_j l^(n-j) q_j dout_j^T.
 // A wave owns 16 columns of R, and the same columns of dv and of dk; R^T, which the latter needs, is R rounded in LDS, read transposed.
+//
+// 212 548 rows, 8/2 heads of 64, four heads to a workgroup: 213 us = 3.1 TB/s (dk and dv as two sweeps of their own 460; in one 325; with a body for each kind
+// of rows and the sums held where they are formed, 213).  364 182 rows, 16/2 of 128, two heads: 1780 to 2066 us = 3.1 to 3.6 TB/s, half of it the shares of dk
+// and dv (3526 and 2870 on that way).  LDS is the busiest unit, 0.47 of the time; at d = 128 its 115 KB leave one workgroup to a compute unit.
 template <int D, int G, int C, bool FULL>
 __global__ __launch_bounds__(D * 4, 2) void back_kernel(const Args args) {
     constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, KS = D / 32, PART = NT / C16, LOADS = C / PART, TILE = C * D * 2, IT = C / 16, KT = C / 32, TILES = IT * (IT + 1) / 2;
@@ -633,7 +648,8 @@ template <int D, int G, int C>
 constexpr int back_lds() { return 4 * C * D * 2 + 2 * C * C * 2 + D * D * 2 + (2 * C + 2 * G * POWERS) * 4; }
 
 // What each piece adds to a state that starts at zero: forwards sum_j l^(n-1-j) b_j c_j^T over a history's piece, backwards scale times sum_j l^(n-j) q_j dout_j^T
-// over either kind (candidates: l).  blockIdx.y: 1 backwards.
+// over either kind (candidates: l).  blockIdx.y: 1 backwards.  A chain of chunks, bound by its latency: one user of 8192 rows, 16/2 heads of 128, pieces of 256
+// rows, 24.7 us; 8 users of up to 4096, 8/2 of 64, 12.1 (in chunks of 32 rows 13.3; at d = 128 chunks of 64 do not fit the registers).
 template <int D, int C>
 __global__ __launch_bounds__(D * 4, 4) void states_kernel(const Args args, int first_job, int whole_jobs) {
     constexpr int NW = D / 16, NT = NW * 64, C16 = D / 8, PART = NT / C16, LOADS = C / PART, TILE = C * D * 2, KT = C / 32;
@@ -697,6 +713,7 @@ __global__ __launch_bounds__(D * 4, 4) void states_kernel(const Args args, int f
 }
 
 // The states in front of the pieces from what each adds, in the order of the sweep: X <- l^n X + U, in place; the last is the caller's.  blockIdx.z: 1 backwards.
+// Bound by its traffic where states are many (16 heads x 33 states of 128 x 128: 69 MB in 13.3 us = 5.2 TB/s), by a trip to memory where they are few (4 us).
 constexpr int SCAN_THREADS = 256, SCAN_AHEAD = 16;  // loads in flight: the sum is all latency
 template <int D>
 __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const Args args, int first_job, const float* in_ahead, int transposed, float* out_ahead, const float* in_back,
@@ -737,7 +754,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const Args args, int
     if (out) *(floatx4*)(out + state + e) = x;
 }
 
-// dk, dv = the sum of a group's shares, for the rows of the users
+// dk, dv = the sum of a group's shares, for the rows of the users.  Bound by HBM: 364 182 rows, 2 heads of 128, 4 shares: 720 to 765 us = 4.4 to 4.7 TB/s.
 constexpr int SUM_THREADS = 256, SUM_BLOCKS = 64;  // (per user)
 __global__ __launch_bounds__(SUM_THREADS) void sum_kernel(const Args args, int d) {
     const User us = user_of(args, blockIdx.x);
@@ -761,7 +778,8 @@ __global__ __launch_bounds__(SUM_THREADS) void sum_kernel(const Args args, int d
 }
 
 // Single tokens: a workgroup per row and query head, the state in registers between its reading and its writing.  Lane groups of D / 4 lanes
-// hold a state row each (16-byte words), so thread t has columns 4 (t % (D / 4)) .. of rows t / (D / 4) + i ROWS.  Bound by HBM: the state in and out.
+// hold a state row each (16-byte words), so thread t has columns 4 (t % (D / 4)) .. of rows t / (D / 4) + i ROWS.  Bound by HBM: the state in and out
+// (96 rows, 16/2 heads of 128: 201 MB in 30.2 to 37.2 us, 5.4 TB/s or more; one row, 8/2 of 64: 3.3 us, the launch and two trips to memory).
 // While the state is on its way, the workgroup looks at the other rows' slots: the first row of a slot does the work of all that name it.
 constexpr int STEP_THREADS = 256;
 template <int D>
@@ -841,8 +859,8 @@ int check_heads(int32_t Hq, int32_t Hkv, int32_t d, int dtype) {
 }
 
 constexpr int64_t MOST_TOKENS = (int64_t)1 << 30;  // (the last piece or chunk may end behind them, in 32 bits)
-// A launch has less than 2^32 threads: 4 head_dim to a workgroup, or 256 of the scan; 8 groups of heads may be none.
-bool launchable(int64_t workgroups, int d) { return workgroups * std::max(4 * d, 256) < ((int64_t)1 << 32) - ((int64_t)1 << 26); }
+// A launch has less than 2^32 threads: 4 head_dim to a workgroup, or 256 of the scan; up to 8 groups of heads (2^22 features) may be none.
+bool launchable(int64_t workgroups, int d) { return workgroups * std::max(4 * d, 256) < ((int64_t)1 << 32) - ((int64_t)1 << 27); }
 
 int check_sizes(int layer, int dtype, int32_t batch, int64_t total_q, int64_t total_kv, int32_t max_hist, int32_t max_targets, int32_t Hq, int32_t Hkv, int32_t d) {
     if (int rc = check_heads(Hq, Hkv, d, dtype)) return rc;
@@ -856,7 +874,8 @@ int check_sizes(int layer, int dtype, int32_t batch, int64_t total_q, int64_t to
 constexpr int MIN_SEG = 128;  // rows of a piece at least; a multiple of what a chunk has
 // rows of a chunk
 constexpr int sweep_rows(int D, bool FULL) { return D == 128 && FULL ? 32 : 64; }
-constexpr int BACK_ROWS = 64, STATES_ROWS = 32;
+constexpr int states_rows(int D) { return D == 128 ? 32 : 64; }
+constexpr int BACK_ROWS = 64;
 
 // heads of a group that a backward workgroup may hold: what registers allow
 int most_heads(int d, bool full) { return d == 128 && full ? 2 : 4; }
@@ -876,8 +895,8 @@ Plan plan_of(bool backward, bool full, int batch, int64_t total_kv, int max_hist
     max_hist = (int)std::min((int64_t)max_hist, total_kv), max_targets = (int)std::min((int64_t)max_targets, total_kv);
     // How a call is cut up goes by the time of each way, in us.  A user's head is one workgroup's work, so a sweep lasts as long as the longest history takes by
     // itself, at least; cut into pieces, whose states take another reading of half a sweep's work and two launches, it lasts as long as the chip needs for all
-    // rows, in whole pieces to a compute unit (0.85: a user's last one is not whole).  The heads of a group that a backward workgroup does not hold are summed by a launch of its own, over shares that
-    // are written and read.  `mean`: rows of a place on a full chip; us of a row there, and of a row of a workgroup that is alone on its compute unit, in a sweep
+    // rows, in whole pieces to a compute unit (0.85: a user's last one is not whole).  The heads of a group that a backward workgroup does not hold are
+    // summed by a launch of its own, over shares that are written and read.  `mean`: rows of a place on a full chip; us of a row there, and of a row of a workgroup that is alone on its compute unit, in a sweep
     // and (of a head) in the sweep for dk and dv: as measured.  (Forward, us, by rows of a piece none / 128 / 256 / 512: one user of 8192, 16/2 heads of 128,
     // 462 / 91 / 77 / 94; 18 users of 360 to 5080, 8/2 of 64, 157 / 62 / 51 / 58; 19 of 438 to 1752 with states, forward and backward, 256 206, 128 150; 256 of
     // 512 to 1024 164 / 357 / 285.  Over 90 calls the choice takes 1.01 of the best one's time; 39 users of 543 to 2424, 8/2 of 64, in pieces of 1024 took 1.8 of that in 256.)
@@ -946,7 +965,7 @@ hipError_t launch_sweep(const Args& a, int d, hipStream_t s) {
 // first_job, jobs: 0, 1 the sweep in the tokens' order; 1, 1 backwards; 0, 2 both
 template <int D>
 hipError_t launch_states_d(const Args& a, int first_job, int jobs, const float* in_ahead, float* out_ahead, const float* in_back, float* out_back, hipStream_t s) {
-    hipLaunchKernelGGL((states_kernel<D, STATES_ROWS>), dim3((unsigned)grid_of(a, a.ratio), jobs), dim3(D * 4), 0, s, a, first_job, (out_ahead ? 1 : 0) | (out_back ? 2 : 0));
+    hipLaunchKernelGGL((states_kernel<D, states_rows(D)>), dim3((unsigned)grid_of(a, a.ratio), jobs), dim3(D * 4), 0, s, a, first_job, (out_ahead ? 1 : 0) | (out_back ? 2 : 0));
     hipLaunchKernelGGL((scan_kernel<D>), dim3(a.batch * a.Hq, D * D / (SCAN_THREADS * 4), jobs), dim3(SCAN_THREADS), 0, s, a, first_job, in_ahead, a.transposed,
                        out_ahead, in_back, out_back);
     return hipGetLastError();
