@@ -99,6 +99,7 @@ class DecayBatch:
 
     def _call(self, dout, dfinal, workspace, stream) -> None:
         back = dout is not None
+        hta.check_on_current_device(self.q, dout, dfinal)
         P = hta._address
         grads = (dout.data_ptr(), self.dq.data_ptr(), self.dk.data_ptr(), self.dv.data_ptr(), P(dfinal), P(self.dstate)) if back else (0,) * 6
         q_offsets, kv_offsets, hist_len, n_targets = self.ints
@@ -129,7 +130,6 @@ class DecayBatch:
         _check("dout", dout, self.q.shape, torch.bfloat16)
         if dstate is not None:
             _check("dstate", dstate, self._state_shape, torch.float32)
-        hta.check_on_current_device(dout, dstate)
         self.prepare_backward()
         self._call(dout, dstate, self.bwd_workspace, stream)
         return self.dq, self.dk, self.dv, self.dstate

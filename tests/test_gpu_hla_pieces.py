@@ -115,3 +115,15 @@ def test_two_batches_take_turns_on_one_stream():
         assert all(x[k] is None or torch.equal(x[k], y[k]) for k in x)
     check(again[0], a)
     check(again[1], b)
+
+
+def test_a_batch_of_another_device_than_the_current_one_is_refused(monkeypatch):
+    s = Sample([20], [2], 4, 2, 32, True, seed=1)
+    b = s.batch()
+    monkeypatch.setattr(hta, "_device_index", lambda: 1)   # (the refusal stands in front of any launch)
+    b.out.fill_(3.0)
+    with pytest.raises(ValueError, match="current GPU"):
+        b.forward()
+    with pytest.raises(ValueError, match="current GPU"):
+        b.backward(s.gpu["dout"])
+    assert (b.out == 3.0).all()
