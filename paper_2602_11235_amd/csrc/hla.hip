@@ -6,7 +6,7 @@
 // in the same direction with the states transposed, and from the last row backwards dv for (k, q, dout) and dk for (v, dout, q), which
 // share the state (one has it transposed) and are one kernel.
 //
-// A workgroup owns a user's head and goes through the tokens in chunks of 64 (or 32).  Inside a chunk, with i, j counted from its start and
+// A workgroup owns a user's head and goes through the tokens in chunks of 64 or 32.  Inside a chunk, with i, j counted from its start and
 // S the state in front of it,
 //   o_i = scale [ l^(i+1) a_i S + sum_(j<=i) l^(i-j) <a_i, b_j> c_j ],    S <- l^n S + sum_j l^(n-1-j) b_j c_j^T:
 // four matrix products.  The floor is HBM's (4 d^2 + 64 d operations per row and head on 8 d bytes), so a row is read once: the
@@ -872,10 +872,13 @@ int check_sizes(int layer, int dtype, int32_t batch, int64_t total_q, int64_t to
 }
 
 constexpr int MIN_SEG = 128;  // rows of a piece at least; a multiple of what a chunk has
-// rows of a chunk
-constexpr int sweep_rows(int D, bool FULL) { return D == 128 && FULL ? 32 : 64; }
+// Rows of a chunk: 64, and 32 where LDS for 64 keeps workgroups off a compute unit that registers would let in.  (us, 64 / 32: forward and backward of 54 users of
+// 1090 rows, 4/2 heads of 32, 117 / 103, of 192 of 197 70.4 / 64.0; backward of 239 users of up to 304, 4/4 of 64, 81.1 / 65.9, of 42 of 1016 97 / 103;
+// forward of 364 182 rows, 16/2 of 128, 1073 / 1032; at d = 64 the forward pass takes the same, and with four heads to a backward workgroup, or at d = 128, 32
+// rows take 1.07 of the time.)
+constexpr int sweep_rows(int D, bool FULL) { return D != 64 && FULL ? 32 : 64; }
+constexpr int back_rows(int D, int G, bool FULL) { return D == 32 || (D == 64 && G <= 2 && FULL) ? 32 : 64; }
 constexpr int states_rows(int D) { return D == 128 ? 32 : 64; }
-constexpr int BACK_ROWS = 64;
 
 // heads of a group that a backward workgroup may hold: what registers allow
 int most_heads(int d, bool full) { return d == 128 && full ? 2 : 4; }
@@ -993,7 +996,7 @@ hipError_t allow_lds(int bytes) {
 }
 template <int D, int G, bool FULL>
 hipError_t launch_back_as(const Args& a, hipStream_t s) {
-    constexpr int C = BACK_ROWS, lds = back_lds<D, G, C>();
+    constexpr int C = back_rows(D, G, FULL), lds = back_lds<D, G, C>();
     if (hipError_t e = allow_lds<back_kernel<D, G, C, FULL>>(lds); e != hipSuccess) return e;
     hipLaunchKernelGGL((back_kernel<D, G, C, FULL>), dim3((unsigned)grid_of(a, a.spread)), dim3(D * 4), lds, s, a);
     return hipGetLastError();
