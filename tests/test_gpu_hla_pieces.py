@@ -127,3 +127,24 @@ def test_a_batch_of_another_device_than_the_current_one_is_refused(monkeypatch):
     with pytest.raises(ValueError, match="current GPU"):
         b.backward(s.gpu["dout"])
     assert (b.out == 3.0).all()
+
+
+@pytest.mark.parametrize("value", (float("nan"), float("inf")))
+@pytest.mark.parametrize("heads", ((4, 2, 32), (4, 4, 64), (4, 2, 64), (8, 2, 64), (4, 2, 128)))
+def test_what_a_row_may_not_see_does_not_reach_it_for_any_heads(heads, value):
+    """Chunks of either length, at either end of one: rows in front of a token (behind it, backwards) do not see that it is not finite."""
+    r = heads[0] // heads[1]
+    for at in (31, 32, 64, 95, 130):
+        s = Sample([150, 80], [3, 2], *heads, True, seed=at)
+        s.v[at, 1, 5] = value
+        out = host(s.batch().forward()[0])
+        assert np.isfinite(out[:at]).all() and np.isfinite(out[:, :r]).all() and np.isfinite(out[153:]).all()
+        assert not np.isfinite(out[at:150, r:2 * r, 5]).all(0).any()
+        s = Sample([150, 80], [3, 2], *heads, True, seed=at)
+        s.dout[at, r, 7] = value
+        got = run(s)
+        for name in ("dk", "dv"):
+            g = host(got[name])
+            assert np.isfinite(g[at + 1:]).all() and np.isfinite(np.delete(g, 1, 1)).all(), name
+        assert not np.isfinite(host(got["dv"])[:at + 1, 1, 7]).all()
+        assert np.isfinite(np.delete(host(got["dq"]), at, 0)).all()
